@@ -36,8 +36,8 @@ def _weights_case(name, dtype, e, n_out, n_in):
     return {"name": name, "op": "weights", "dtype": dtype, "experts": e, "n_out": n_out, "n_in": n_in}
 
 
-def _gemm_case(name, out, tokens, e, k, n_in, n_out, gather=False, gamma=0.0, skew="normal", skew_param=1.0):
-    return {"name": name, "op": "gemm", "out": out, "tokens": tokens, "experts": e, "top_k": k, "n_in": n_in,
+def _gemm_case(name, tokens, e, k, n_in, n_out, gather=False, gamma=0.0, skew="normal", skew_param=1.0):
+    return {"name": name, "op": "gemm", "tokens": tokens, "experts": e, "top_k": k, "n_in": n_in,
             "n_out": n_out, "gather": gather, "gamma": gamma, "skew": skew, "skew_param": skew_param}
 
 
@@ -57,13 +57,13 @@ def listed():
         # loading fp32 experts whose sizes divide nothing
         _weights_case("weights_f32_odd", "f32", 7, 1000, 1416),
         # one projection of a single token's eight experts: latency and the weight stream
-        _gemm_case("gemm_1_token", "bf16", 1, 64, 8, 2048, 1024, skew="zipf", skew_param=1.1),
-        # an expert that all tokens share (a dense product) in a decoding batch, sizes that are no multiples of 128, fp32 sums out
-        _gemm_case("gemm_shared_odd_f32", "f32", 203, 1, 1, 2056, 5640),
+        _gemm_case("gemm_1_token", 1, 64, 8, 2048, 1024, skew="zipf", skew_param=1.1),
+        # an expert that all tokens share (a dense product) in a decoding batch, sizes that are no multiples of 128
+        _gemm_case("gemm_shared_odd", 203, 1, 1, 2056, 5640),
         # one projection of a skewed prompt batch, rows fetched through the plan
-        _gemm_case("gemm_4096_ragged", "bf16", 4096, 64, 8, 2048, 1024, gather=True, gamma=1.0, skew="zipf", skew_param=1.1),
+        _gemm_case("gemm_4096_ragged", 4096, 64, 8, 2048, 1024, gather=True, gamma=1.0, skew="zipf", skew_param=1.1),
         # few wide experts, long sums: the matrix cores bind
-        _gemm_case("gemm_8192_wide", "bf16", 8192, 8, 2, 14336, 4096, gamma=1.0, skew_param=1.5),
+        _gemm_case("gemm_8192_wide", 8192, 8, 2, 14336, 4096, gamma=1.0, skew_param=1.5),
         # decoding a small batch with few, wide experts: streams nearly all weights for sixteen tokens
         _ffn_case("ffn_16_wide", 16, 4096, 8, 2, 14336, skew_param=0.5),
         # a short ragged prompt on a layer whose counts divide nothing
@@ -110,7 +110,7 @@ def draw(rng):
             if op == "gemm":
                 if rng.random() < 0.5:
                     a, b = b, a
-                c = _gemm_case("", rng.choice(["bf16", "bf16", "f32"]), n, e, k, a, b, rng.random() < 0.5, gamma, skew, param)
+                c = _gemm_case("", n, e, k, a, b, rng.random() < 0.5, gamma, skew, param)
             else:
                 c = _ffn_case("", n, a, e, k, b, gamma, skew, param)
             mats = 3 if op == "ffn" else 1
@@ -250,7 +250,7 @@ def prepare(case, seed):
         x = normal((t if case["gather"] else s["rows"], d), 1.0, torch.bfloat16)
         s["xq"], s["xs"] = (v.view(torch.uint8) for v in _quantize_rows(x))
         s["w"] = experts(e, h, d, d ** -0.5)
-        s["y"] = torch.zeros((s["rows"], h), dtype=DTYPES[case["out"]], device="cuda")
+        s["y"] = torch.zeros((s["rows"], h), dtype=torch.bfloat16, device="cuda")
     else:
         s["x"] = normal((t, d), 1.0, torch.bfloat16)
         s["gate"], s["up"], s["down"] = experts(e, h, d, d ** -0.5), experts(e, h, d, d ** -0.5), experts(e, d, h, h ** -0.5)
@@ -301,8 +301,7 @@ def run(s):
         return s["q"].view(torch.float8_e4m3fn), s["scale"]
     if case["op"] == "gemm":
         if "gemm" not in s:  # what a program sets up once
-            out = capmoe.DTYPE_BF16 if case["out"] == "bf16" else capmoe.DTYPE_F32
-            s["gemm"] = capmoe.make_gemm(s["rows"], case["n_in"], case["n_out"], case["experts"], out,
+            s["gemm"] = capmoe.make_gemm(s["rows"], case["n_in"], case["n_out"], case["experts"],
                                          src_rows=case["tokens"] if case["gather"] else 0)
             s["workspace"] = torch.empty(capmoe.moe_gemm_query(s["gemm"]), dtype=torch.uint8, device="cuda")
         capmoe.moe_grouped_gemm_fp8(s["gemm"], s["xq"], s["xs"], s["row_token"] if case["gather"] else None,
@@ -329,8 +328,7 @@ def work(case):
     rows, active = sum(counts), sum(c > 0 for c in counts)
     d, h, t = case["n_in"], case["n_out"], case["tokens"]
     if case["op"] == "gemm":
-        out = 2 if case["out"] == "bf16" else 4
-        return {"bytes": active * d * h + (min(rows, t) if case["gather"] else rows) * d + rows * h * out, "flops": 2 * rows * d * h}
+        return {"bytes": active * d * h + (min(rows, t) if case["gather"] else rows) * d + rows * h * 2, "flops": 2 * rows * d * h}
     return {"bytes": 3 * active * d * h + min(rows, t) * d * 2 + rows * d * 2, "flops": 6 * rows * d * h}
 
 
