@@ -241,6 +241,94 @@ int moe_layer_forward(const moe_desc_t* desc, const void* x, const float* w_rout
                       size_t workspace_bytes, void* stream);
 
 /*
+ * Experts in 8 bits (OCP e4m3 values with power-of-two scales, which the matrix instructions of gfx950 apply themselves).
+ *
+ * The 8-bit form of a matrix of c columns has rows of pitch = 128 * ceil(c / 128) bytes, one e4m3 value each, zero behind
+ * column c, and one scale byte per row and 128 columns in rows of scale_pitch = 4 * ceil(c / 512) bytes, zero behind the
+ * last: the value is e4m3 * 2^(byte - 127).  Expert weights [E,n,c] have n filled up to a multiple of 128 with rows of zeros
+ * and one scale byte per 128 rows x 128 columns: values [E, 128 * ceil(n / 128), pitch], scales [E, ceil(n / 128),
+ * scale_pitch].  Values are 16-byte aligned, scales 4-byte aligned.
+ *   Quantising: the byte of a block is the smallest b >= 0 with amax <= 448 * 2^(b - 127), amax over the block's finite
+ *   values; every value is divided by 2^(b - 127) (exactly) and rounded once to e4m3, to nearest even; NaN and infinities
+ *   become NaN (0x7F).  So a value is off by at most 2^-4 of itself, or by 2^-10 * 2^(b - 127) where that is more.
+ */
+
+/* pitch and scale_pitch of an 8-bit matrix of `cols` columns, in bytes (host only; either may be NULL). */
+int moe_fp8_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch);
+
+/*
+ * Rows of activations to 8 bits, on the way permuted if row_token is given (moe_dispatch and quantising in one pass):
+ * q[r,:], scale[r,:] from x[row_token ? row_token[r] : r, :] for r < n_rows, and r < *row_count if that is given
+ * (device; expert_offset + E holds the rows of a plan).  Rows behind stay untouched.
+ *   dtype MOE_DTYPE_* of x [*,cols]; rows are moved in 16-byte pieces: cols a multiple of 8 (bf16) or 4 (fp32),
+ *   x and q 16-byte aligned, scale 4-byte aligned.
+ * n_rows == 0 enqueues nothing, and its arrays may be null.  Fewer than 2^31 blocks of 128, else MOE_ERR_UNSUPPORTED.
+ */
+int moe_quantize_rows(int dtype, const void* x, int64_t n_rows, int32_t cols, const int32_t* row_token,
+                      const int32_t* row_count, void* q, uint8_t* scale, void* stream);
+
+/* Expert weights w [n_experts, n_out, n_in] in dtype to 8 bits, padding included.  n_in as `cols` above. */
+int moe_quantize_weights(int dtype, const void* w, int32_t n_experts, int32_t n_out, int32_t n_in, void* q,
+                         uint8_t* scale, void* stream);
+
+/* One product of 8-bit rows and 8-bit expert weights (host memory, plain data). */
+typedef struct {
+    int32_t max_rows;   /* most rows of y: expert_offset[E] <= max_rows                                        */
+    int32_t src_rows;   /* rows of x when they are fetched through row_token; ignored without a row_token      */
+    int32_t n_experts;  /* E, at most 256                                                                      */
+    int32_t n_in;       /* columns of x and of a weight row, at most 2^21                                      */
+    int32_t n_out;      /* columns of y and rows of an expert's weights: a multiple of 8, at most 2^21         */
+} moe_gemm_t;
+
+/* Workspace of moe_grouped_gemm_fp8 (host only). */
+int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes);
+
+/*
+ * Matrix product grouped by expert: for the rows r of expert e, expert_offset[e] <= r < expert_offset[e+1],
+ *   y[r,n] = sum_k x[row_token ? row_token[r] : r, k] * w[e,n,k]          y [max_rows,n_out] bf16
+ * of the values that x (8-bit rows) and w (8-bit weights) stand for, accumulated in fp32 on the matrix cores, rounded once.
+ * Offsets are ascending from 0 (device); an expert may have no rows.  Rows at or behind expert_offset[E] stay untouched.
+ * n_experts = 1 is a plain product (an expert that all tokens share).  With row_token, x must be smaller than 4 GiB, else
+ * MOE_ERR_UNSUPPORTED.  The same call gives the same bits; the order of a row's sums may differ with the number of rows
+ * of its expert and of the batch.  y must be 16-byte aligned.
+ */
+int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x_scale, const int32_t* row_token,
+                         const int32_t* expert_offset, const void* w, const uint8_t* w_scale, void* y, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* The 8-bit weights of a layer's experts: gate and up [E,h,d], down [E,d,h] (device pointers, host struct). */
+typedef struct {
+    const void* gate;
+    const uint8_t* gate_scale;
+    const void* up;
+    const uint8_t* up_scale;
+    const void* down;
+    const uint8_t* down_scale;
+} moe_fp8_experts_t;
+
+/* Workspace that is enough for any of the three calls below and any call of moe_query's list (host only). */
+int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes);
+
+/*
+ * moe_grouped_ffn, moe_dispatch_ffn and moe_layer_forward with 8-bit experts.  desc->dtype is MOE_DTYPE_BF16 (the type of
+ * xp / x, yp and y); any other is MOE_ERR_UNSUPPORTED.  d is a multiple of 8, h any number; d and h at most 2^21.  The
+ * activations are quantised on the way: xp / x by rows, and the hidden activation, rounded to bf16 once, by rows too.
+ * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp8 and moe_layer_forward_fp8: N * d < 2^31.
+ * Under a profile table the quantising of x counts as MOE_KERNEL_DISPATCH.
+ */
+int moe_grouped_ffn_fp8(const moe_desc_t* desc, const void* xp, const int32_t* expert_offset,
+                        const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
+                        void* stream);
+int moe_dispatch_ffn_fp8(const moe_desc_t* desc, const void* x, const int32_t* expert_offset, const int32_t* row_token,
+                         const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
+                         void* stream);
+int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_router, const float* bias,
+                          const moe_fp8_experts_t* experts, const uint8_t* token_class, uint32_t seed, float* logits,
+                          float* scores, int32_t* topk_idx, float* topk_score, int32_t* expert_count,
+                          int32_t* seg_count, int32_t* expert_offset, int32_t* row_token, float* row_weight,
+                          int32_t* pair_row, void* yp, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Profiling hook (instrumentation, not part of the method).  The table is the caller's (host memory); the
  * library keeps only a pointer to it, per host thread, between moe_profile_attach(table) and
  * moe_profile_attach(NULL).  While a table is attached to the calling thread, every launch of kernel id k by

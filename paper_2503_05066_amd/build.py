@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libcapmoe.so")
 
-SOURCES = ["api.hip", "route.hip", "router_mfma.hip", "drop.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip", "probe.hip"]
+SOURCES = ["api.hip", "route.hip", "router_mfma.hip", "drop.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip", "probe.hip",
+           "quantize.hip", "fp8_thin.hip", "api_fp8.hip"]
 # the packed-fp32 feature is switched off for all device code; the first sixteen words of a kernel's arguments arrive in
 # registers (a token through 64 experts x 2048 x 1024: 38.3 -> 37.7 us); the router file must not contract
 # multiplies and adds (its softmax is a fixed sequence of individually rounded operations)

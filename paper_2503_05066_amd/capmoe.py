@@ -32,6 +32,18 @@ class MoeDesc(ctypes.Structure):
     ]
 
 
+class MoeGemm(ctypes.Structure):
+    """moe_gemm_t of include/capmoe.h."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("max_rows", "src_rows", "n_experts", "n_in", "n_out")]
+
+
+class MoeFp8Experts(ctypes.Structure):
+    """moe_fp8_experts_t of include/capmoe.h."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "gate_scale", "up", "up_scale", "down", "down_scale")]
+
+
 KERNELS = ("router_logits", "softmax_topk", "drop_prepare", "drop_select", "drop_emit", "dispatch", "ffn_schedule",
            "ffn_gate_up", "ffn_down", "combine", "drop_limit")
 
@@ -93,6 +105,19 @@ def load():
         lib.moe_ffn_schedule_query.restype = i32
         lib.moe_probe_mfma_bf16.argtypes = [i32, i32, i32, vp, ctypes.POINTER(ctypes.c_int64), vp]
         lib.moe_probe_mfma_bf16.restype = i32
+        gp, ep, i64 = ctypes.POINTER(MoeGemm), ctypes.POINTER(MoeFp8Experts), ctypes.c_int64
+        lib.moe_fp8_query.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
+        lib.moe_quantize_rows.argtypes = [i32, vp, i64, ctypes.c_int32, vp, vp, vp, vp, vp]
+        lib.moe_quantize_weights.argtypes = [i32, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp, vp]
+        lib.moe_gemm_query.argtypes = [gp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_grouped_gemm_fp8.argtypes = [gp] + [vp] * 8 + [sz, vp]
+        lib.moe_query_fp8.argtypes = [dp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_grouped_ffn_fp8.argtypes = [dp, vp, vp, ep, vp, vp, sz, vp]
+        lib.moe_dispatch_ffn_fp8.argtypes = [dp, vp, vp, vp, ep, vp, vp, sz, vp]
+        lib.moe_layer_forward_fp8.argtypes = [dp, vp, vp, vp, ep, vp, ctypes.c_uint32] + [vp] * 13 + [sz, vp]
+        for f in ("moe_fp8_query", "moe_quantize_rows", "moe_quantize_weights", "moe_gemm_query", "moe_grouped_gemm_fp8",
+                  "moe_query_fp8", "moe_grouped_ffn_fp8", "moe_dispatch_ffn_fp8", "moe_layer_forward_fp8"):
+            getattr(lib, f).restype = i32
         for f in ("moe_query", "moe_route_topk", "moe_route_topk_static", "moe_capacity_drop", "moe_capacity_drop_ranked", "moe_dispatch",
                   "moe_grouped_ffn",
                   "moe_dispatch_ffn", "moe_combine"):
@@ -203,6 +228,144 @@ def moe_layer_forward(desc, x, w_router, bias, w_gate, w_up, w_down, token_class
     return buf.y
 
 
+def moe_fp8_query(cols: int):
+    """(pitch, scale_pitch) in bytes of an 8-bit matrix of this many columns; host only."""
+    pitch, scale_pitch = ctypes.c_int32(), ctypes.c_int32()
+    _check(load().moe_fp8_query(int(cols), ctypes.byref(pitch), ctypes.byref(scale_pitch)), "moe_fp8_query")
+    return pitch.value, scale_pitch.value
+
+
+def _fits(ok, what):
+    """The quantising calls read their sizes off the tensors, so a tensor that does not fit them is refused here."""
+    if not ok:
+        raise ValueError(what)
+
+
+def _value_dtype(t, dims, what):
+    dtype = {"torch.float32": DTYPE_F32, "torch.bfloat16": DTYPE_BF16}.get(str(t.dtype))
+    _fits(dtype is not None and t.dim() == dims and t.is_contiguous(), f"{what}: a dense bf16 or fp32 tensor of {dims} dimensions")
+    return dtype
+
+
+def _fits_fp8(t, shape, what):
+    _fits(tuple(t.shape) == shape and t.element_size() == 1 and t.is_contiguous(), f"{what}: a dense tensor of {shape} bytes")
+
+
+def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
+    """x [*, cols] (bf16 or fp32) into the 8-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
+    dtype = _value_dtype(x, 2, "x")
+    n_rows, cols = q.shape[0], x.shape[1]
+    pitch, scale_pitch = moe_fp8_query(cols)
+    _fits_fp8(q, (n_rows, pitch), "q")
+    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+    if row_token is None:
+        _fits(x.shape[0] >= n_rows, "x: a row for every row of q")
+    else:
+        _fits(str(row_token.dtype) == "torch.int32" and row_token.numel() >= n_rows and row_token.is_contiguous(),
+              "row_token: a dense int32 for every row of q")
+    _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
+                                    _stream(stream)), "moe_quantize_rows")
+
+
+def moe_quantize_weights(w, q, scale, stream=None):
+    """w [E, n_out, n_in] (bf16 or fp32) into the 8-bit weights q, scale (see fp8_weight_buffers)."""
+    dtype = _value_dtype(w, 3, "w")
+    e, n_out, n_in = w.shape
+    pitch, scale_pitch = moe_fp8_query(n_in)
+    blocks = -(-n_out // 128)
+    _fits_fp8(q, (e, blocks * 128, pitch), "q")
+    _fits_fp8(scale, (e, blocks, scale_pitch), "scale")
+    _check(load().moe_quantize_weights(dtype, _ptr(w), e, n_out, n_in, _ptr(q), _ptr(scale), _stream(stream)),
+           "moe_quantize_weights")
+
+
+def fp8_row_buffers(n_rows: int, cols: int, device="cuda"):
+    """(values, scales) of the 8-bit form of [n_rows, cols], uninitialised."""
+    import torch
+
+    pitch, scale_pitch = moe_fp8_query(cols)
+    return (torch.empty((n_rows, pitch), dtype=torch.uint8, device=device),
+            torch.empty((n_rows, scale_pitch), dtype=torch.uint8, device=device))
+
+
+def fp8_weight_buffers(n_experts: int, n_out: int, n_in: int, device="cuda"):
+    """(values, scales) of the 8-bit form of expert weights [n_experts, n_out, n_in], uninitialised."""
+    import torch
+
+    pitch, scale_pitch = moe_fp8_query(n_in)
+    blocks = -(-n_out // 128)
+    return (torch.empty((n_experts, blocks * 128, pitch), dtype=torch.uint8, device=device),
+            torch.empty((n_experts, blocks, scale_pitch), dtype=torch.uint8, device=device))
+
+
+class Fp8Experts:
+    """The 8-bit weights of a layer's experts (keeps the tensors alive; allocation and marshalling only)."""
+
+    def __init__(self, gate, gate_scale, up, up_scale, down, down_scale):
+        self.tensors = (gate, gate_scale, up, up_scale, down, down_scale)
+        self.struct = MoeFp8Experts(*[t.data_ptr() for t in self.tensors])
+
+    @classmethod
+    def quantized(cls, w_gate, w_up, w_down, stream=None):
+        """From w_gate, w_up [E,h,d] and w_down [E,d,h] in bf16 or fp32 (as at model load)."""
+        tensors = []
+        for w in (w_gate, w_up, w_down):
+            q, scale = fp8_weight_buffers(*w.shape, device=w.device)
+            moe_quantize_weights(w, q, scale, stream)
+            tensors += [q, scale]
+        return cls(*tensors)
+
+
+def make_gemm(max_rows, n_in, n_out, n_experts=1, src_rows=0) -> MoeGemm:
+    return MoeGemm(max_rows, src_rows, n_experts, n_in, n_out)
+
+
+def moe_gemm_query(gemm: MoeGemm) -> int:
+    """Workspace bytes of moe_grouped_gemm_fp8; host only."""
+    ws = ctypes.c_size_t()
+    _check(load().moe_gemm_query(ctypes.byref(gemm), ctypes.byref(ws)), "moe_gemm_query")
+    return ws.value
+
+
+def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace, stream=None):
+    _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), _ptr(x), _ptr(x_scale), _ptr(row_token), _ptr(expert_offset),
+                                       _ptr(w), _ptr(w_scale), _ptr(y), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream(stream)),
+           "moe_grouped_gemm_fp8")
+
+
+def moe_query_fp8(desc: MoeDesc) -> int:
+    """Workspace bytes of a layer with 8-bit experts; host only."""
+    ws = ctypes.c_size_t()
+    _check(load().moe_query_fp8(ctypes.byref(desc), ctypes.byref(ws)), "moe_query_fp8")
+    return ws.value
+
+
+def moe_grouped_ffn_fp8(desc, xp, expert_offset, experts: Fp8Experts, yp, workspace, stream=None):
+    _check(load().moe_grouped_ffn_fp8(ctypes.byref(desc), _ptr(xp), _ptr(expert_offset), ctypes.byref(experts.struct),
+                                      _ptr(yp), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream(stream)), "moe_grouped_ffn_fp8")
+
+
+def moe_dispatch_ffn_fp8(desc, x, expert_offset, row_token, experts: Fp8Experts, yp, workspace, stream=None):
+    _check(load().moe_dispatch_ffn_fp8(ctypes.byref(desc), _ptr(x), _ptr(expert_offset), _ptr(row_token),
+                                       ctypes.byref(experts.struct), _ptr(yp), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream(stream)),
+           "moe_dispatch_ffn_fp8")
+
+
+def moe_layer_forward_fp8(desc, x, w_router, bias, experts: Fp8Experts, token_class, seed, buf, stream=None):
+    """The whole layer with 8-bit experts, into the buffers of a LayerBuffers made with fp8=True."""
+    ws = buf.workspace
+    _check(load().moe_layer_forward_fp8(
+        ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(bias), ctypes.byref(experts.struct), _ptr(token_class),
+        int(seed) & 0xFFFFFFFF, _ptr(buf.logits), _ptr(buf.scores), _ptr(buf.topk_idx), _ptr(buf.topk_score),
+        _ptr(buf.expert_count), _ptr(buf.seg_count), _ptr(buf.expert_offset), _ptr(buf.row_token),
+        _ptr(buf.row_weight), _ptr(buf.pair_row), _ptr(buf.yp), _ptr(buf.y), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(stream)), "moe_layer_forward_fp8")
+    return buf.y
+
+
 def moe_profile_attach(table: "MoeProfile | None"):
     """Attach the caller's profile table to this thread (None detaches).  The caller keeps the table alive."""
     _check(load().moe_profile_attach(ctypes.byref(table) if table is not None else None), "moe_profile_attach")
@@ -231,11 +394,13 @@ def moe_probe_mfma_bf16(blocks: int, iterations: int, sink, random_operands: boo
 class LayerBuffers:
     """Device buffers of one layer call, sized by moe_query (allocation only, no arithmetic)."""
 
-    def __init__(self, desc: MoeDesc, device="cuda"):
+    def __init__(self, desc: MoeDesc, device="cuda", fp8=False):
         import torch
 
         self.desc = desc
         self.cap, self.slots, self.max_rows, self.workspace_bytes = moe_query(desc)
+        if fp8:  # for the calls with 8-bit experts as well
+            self.workspace_bytes = moe_query_fp8(desc)
         n, e, k, d = desc.n_tokens, desc.n_experts, desc.top_k + desc.overselect, desc.d_model
         blocks = desc.device_groups if desc.capacity_scope in (SCOPE_LOCAL, SCOPE_LOCAL_DEVICE) else 1
         act = torch.bfloat16 if desc.dtype == DTYPE_BF16 else torch.float32

@@ -1,0 +1,278 @@
+// The entry points of the 8-bit experts: argument validation, workspace layout, the calls' launches.
+#include <algorithm>
+
+#include "ffn_tile.h"
+#include "fp8.h"
+
+namespace capmoe {
+
+// Workspace of a layer's FFN, or of one product (h == 0: no quantised x, no hidden activation).
+struct Fp8Workspace {
+    FfnWorkspace f;         // hidden: [P_max, h filled up] bf16
+    void* xq;               // [rows of x, pitch]
+    uint8_t* xs;
+    size_t bytes;
+};
+
+static Fp8Workspace gemm_workspace(const Fp8Gemm& g, void* base) {
+    Fp8Workspace w;
+    size_t off = 0;
+    w.f.hidden = nullptr, w.xq = nullptr, w.xs = nullptr;
+    place_schedule(w.f, (char*)base, off, g.experts, g.max_rows, true, false);
+    w.bytes = off;
+    return w;
+}
+
+// `reserve`: bytes at the start that an earlier step of the layer may still use when the schedule is built
+static Fp8Workspace ffn_fp8_workspace(const moe_desc_t& d, const Sizes& s, size_t reserve, void* base) {
+    Fp8Workspace w;
+    char* p = (char*)base;
+    size_t off = 0;
+    const int64_t rows = std::max<int64_t>(s.max_rows, 1);
+    w.f.hidden = p + off;
+    off += align256((size_t)rows * fp8_pitch(d.d_hidden) * 2);
+    const int64_t x_rows = std::max<int64_t>(rows, d.n_tokens);
+    w.xq = p + off;
+    off += align256((size_t)x_rows * fp8_pitch(d.d_model));
+    w.xs = (uint8_t*)(p + off);
+    off += align256((size_t)x_rows * fp8_scale_pitch(d.d_model));
+    off = std::max(off, align256(reserve));
+    place_schedule(w.f, p, off, d.n_experts, s.max_rows, true, false);
+    w.bytes = off;
+    return w;
+}
+
+// The tile schedule's arguments for one product or two on the same tiles.
+static FfnScheduleArgs schedule_args(const FfnWorkspace& ws, const Fp8Gemm& first, bool swiglu, const Fp8Gemm* second, int cus) {
+    FfnScheduleArgs a;
+    a.enabled = 1;
+    a.E = first.experts;
+    a.big_sh = 8;
+    a.small_sh = 6;
+    static_assert(kFfnTileM == 1 << 8 && kFfnTileSmall == 1 << 6, "tile heights");
+    a.small_max = ws.small_max;
+    a.cus = cus;
+    a.L = tile_list_args(ws, true);
+    auto columns = [](const Fp8Gemm& g, bool narrow) { return narrow || g.n_pad % 256 != 0 ? g.n_pad / 128 : g.n_pad / 256; };
+    const int c1 = columns(first, swiglu);
+    a.first = SplitArgs{ws.split_hdr, ws.split_counter, c1, c1, std::min(first.pitch / kFp8Block, kFfnSplitMinK - 1)};
+    a.second = a.first;
+    if (second) {
+        const int c2 = columns(*second, false);
+        a.second = SplitArgs{ws.split_hdr + kFfnSplitHdr, ws.split_counter + 2 * kFfnSplitUnits, c2, c2,
+                             std::min(second->pitch / kFp8Block, kFfnSplitMinK - 1)};
+    }
+    return a;
+}
+
+static int validate_gemm(const moe_gemm_t* g) {
+    if (!g || g->max_rows < 0 || g->src_rows < 0 || g->n_experts < 1 || g->n_in < 1 || g->n_out < 1) return MOE_ERR_INVALID_ARG;
+    if (g->n_experts > kMaxExperts || g->n_in > kFp8MaxWidth || g->n_out > kFp8MaxWidth || g->n_out % 8 != 0) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+static bool misaligned4(const void* p) { return ((uintptr_t)p & 3) != 0; }
+
+static int validate_fp8(const moe_desc_t* d) {
+    const int v = validate(d);
+    if (v != MOE_OK) return v;
+    if (d->dtype != MOE_DTYPE_BF16 || d->d_model > kFp8MaxWidth || d->d_hidden > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (derive(*d).max_rows >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+static int validate_experts(const moe_fp8_experts_t* w) {
+    if (!w || !w->gate || !w->gate_scale || !w->up || !w->up_scale || !w->down || !w->down_scale) return MOE_ERR_INVALID_ARG;
+    if (misaligned16(w->gate) || misaligned16(w->up) || misaligned16(w->down)) return MOE_ERR_INVALID_ARG;
+    if (misaligned4(w->gate_scale) || misaligned4(w->up_scale) || misaligned4(w->down_scale)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+static bool weights_stream(double bytes) { return bytes > (double)(320ull << 20); }
+
+// The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows.
+static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8Workspace& ws, const void* x,
+                                 const int32_t* row_token, const int32_t* expert_offset, const moe_fp8_experts_t& w, void* yp,
+                                 bool schedule_ready, hipStream_t st) {
+    const int hp = fp8_pitch(d.d_hidden);
+    const Fp8Gemm up = fp8_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp8_gemm(d.n_experts, s.max_rows, hp, d.d_model);
+    if (!schedule_ready) launch_ffn_schedule(expert_offset, schedule_args(ws.f, up, true, &down, compute_units()), st);
+    const bool stream = weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
+    const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
+    {
+        ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
+        launch_fp8_thin(up, ws.f, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden, stream, st);
+    }
+    ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
+    launch_fp8_thin(down, ws.f, ws.f.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
+    return hipGetLastError();
+}
+
+}  // namespace capmoe
+
+using namespace capmoe;
+
+static int ffn_fp8_impl(const moe_desc_t* desc, const void* x, const int32_t* row_token, const int32_t* expert_offset,
+                        const moe_fp8_experts_t* experts, void* yp, const Fp8Workspace& ws, bool schedule_ready, void* stream) {
+    return launch_ffn_fp8(*desc, derive(*desc), ws, x, row_token, expert_offset, *experts, yp, schedule_ready,
+                          (hipStream_t)stream) == hipSuccess
+               ? MOE_OK
+               : MOE_ERR_HIP;
+}
+
+static int ffn_fp8_checked(const moe_desc_t* desc, const void* x, const int32_t* row_token, const int32_t* expert_offset,
+                           const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes, void* stream) {
+    const int v = validate_fp8(desc);
+    if (v != MOE_OK) return v;
+    if (!x || !expert_offset || !yp || !workspace) return MOE_ERR_INVALID_ARG;
+    if (misaligned16(x) || misaligned16(yp) || ((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
+    const int w = validate_experts(experts);
+    if (w != MOE_OK) return w;
+    if (row_token && (uint64_t)desc->n_tokens * (uint64_t)desc->d_model >= (1ull << 31)) return MOE_ERR_UNSUPPORTED;
+    const Sizes s = derive(*desc);
+    const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, 0, workspace);
+    if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (s.max_rows == 0) return MOE_OK;
+    return ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, false, stream);
+}
+
+extern "C" {
+
+int moe_fp8_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch) {
+    if (cols < 1) return MOE_ERR_INVALID_ARG;
+    if (cols > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (pitch) *pitch = fp8_pitch(cols);
+    if (scale_pitch) *scale_pitch = fp8_scale_pitch(cols);
+    return MOE_OK;
+}
+
+static int quantize_checks(int dtype, int32_t cols) {
+    if ((dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16) || cols < 1) return MOE_ERR_INVALID_ARG;
+    if (cols > kFp8MaxWidth || cols % (dtype == MOE_DTYPE_BF16 ? 8 : 4) != 0) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+int moe_quantize_rows(int dtype, const void* x, int64_t n_rows, int32_t cols, const int32_t* row_token,
+                      const int32_t* row_count, void* q, uint8_t* scale, void* stream) {
+    const int v = quantize_checks(dtype, cols);
+    if (v != MOE_OK) return v;
+    if (n_rows < 0) return MOE_ERR_INVALID_ARG;
+    if (n_rows == 0) return MOE_OK;
+    if (!x || !q || !scale || misaligned16(x) || misaligned16(q) || misaligned4(scale)) return MOE_ERR_INVALID_ARG;
+    if (n_rows >= (int64_t)1 << 31 || n_rows * fp8_blocks(cols) >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
+    return launch_quantize_rows(dtype, x, n_rows, cols, row_token, row_count, q, scale, (hipStream_t)stream) == hipSuccess
+               ? MOE_OK
+               : MOE_ERR_HIP;
+}
+
+int moe_quantize_weights(int dtype, const void* w, int32_t n_experts, int32_t n_out, int32_t n_in, void* q,
+                         uint8_t* scale, void* stream) {
+    const int v = quantize_checks(dtype, n_in);
+    if (v != MOE_OK) return v;
+    if (n_experts < 1 || n_out < 1) return MOE_ERR_INVALID_ARG;
+    if (n_out > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (!w || !q || !scale || misaligned16(w) || misaligned16(q) || misaligned4(scale)) return MOE_ERR_INVALID_ARG;
+    if ((int64_t)fp8_blocks(n_out) * fp8_blocks(n_in) >= ((int64_t)1 << 31) / n_experts) return MOE_ERR_UNSUPPORTED;
+    return launch_quantize_weights(dtype, w, n_experts, n_out, n_in, q, scale, (hipStream_t)stream) == hipSuccess ? MOE_OK
+                                                                                                                   : MOE_ERR_HIP;
+}
+
+int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes) {
+    const int v = validate_gemm(gemm);
+    if (v != MOE_OK) return v;
+    if (workspace_bytes) *workspace_bytes = gemm_workspace(fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out), nullptr).bytes;
+    return MOE_OK;
+}
+
+int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x_scale, const int32_t* row_token,
+                         const int32_t* expert_offset, const void* w, const uint8_t* w_scale, void* y, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    const int v = validate_gemm(gemm);
+    if (v != MOE_OK) return v;
+    if (!x || !x_scale || !expert_offset || !w || !w_scale || !y || !workspace) return MOE_ERR_INVALID_ARG;
+    if (misaligned16(x) || misaligned16(w) || misaligned16(y) || misaligned4(x_scale) || misaligned4(w_scale)) return MOE_ERR_INVALID_ARG;
+    if (((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
+    const Fp8Gemm g = fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
+    if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
+    const Fp8Workspace ws = gemm_workspace(g, workspace);
+    if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (gemm->max_rows == 0) return MOE_OK;
+    hipStream_t st = (hipStream_t)stream;
+    launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
+    launch_fp8_thin(g, ws.f, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
+                    weights_stream((double)g.experts * g.pitch * g.n_pad), st);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes) {
+    const int v = validate_fp8(desc);
+    if (v != MOE_OK) return v;
+    size_t other = 0;
+    const int q = moe_query(desc, nullptr, nullptr, nullptr, &other);
+    if (q != MOE_OK) return q;
+    const Sizes s = derive(*desc);
+    const size_t mine = ffn_fp8_workspace(*desc, s, drop_workspace(*desc, s, nullptr).bytes, nullptr).bytes;
+    if (workspace_bytes) *workspace_bytes = std::max(mine, other);
+    return MOE_OK;
+}
+
+int moe_grouped_ffn_fp8(const moe_desc_t* desc, const void* xp, const int32_t* expert_offset,
+                        const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    return ffn_fp8_checked(desc, xp, nullptr, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+}
+
+int moe_dispatch_ffn_fp8(const moe_desc_t* desc, const void* x, const int32_t* expert_offset, const int32_t* row_token,
+                         const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+    if (!row_token) return MOE_ERR_INVALID_ARG;
+    return ffn_fp8_checked(desc, x, row_token, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+}
+
+int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_router, const float* bias,
+                          const moe_fp8_experts_t* experts, const uint8_t* token_class, uint32_t seed, float* logits,
+                          float* scores, int32_t* topk_idx, float* topk_score, int32_t* expert_count,
+                          int32_t* seg_count, int32_t* expert_offset, int32_t* row_token, float* row_weight,
+                          int32_t* pair_row, void* yp, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    // every check first, so that a refusal leaves nothing enqueued
+    const int v = validate_fp8(desc);
+    if (v != MOE_OK) return v;
+    const Sizes s = derive(*desc);
+    if (!expert_count || !seg_count || !expert_offset || !workspace) return MOE_ERR_INVALID_ARG;
+    if (((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
+    if (desc->n_tokens > 0) {
+        if (!x || !w_router || !logits || !scores || !topk_idx || !topk_score || !pair_row || !yp || !y || !row_weight)
+            return MOE_ERR_INVALID_ARG;
+        if (misaligned16(x) || misaligned16(w_router) || misaligned16(yp) || misaligned16(y) || misaligned16(scores) ||
+            misaligned16(topk_idx) || misaligned16(pair_row))
+            return MOE_ERR_INVALID_ARG;
+        if ((uint64_t)desc->n_tokens * (uint64_t)desc->d_model >= (1ull << 31)) return MOE_ERR_UNSUPPORTED;
+    }
+    if (s.max_rows > 0) {
+        if (!row_token) return MOE_ERR_INVALID_ARG;
+        const int w = validate_experts(experts);
+        if (w != MOE_OK) return w;
+    }
+    size_t need = 0;
+    const int q = moe_query_fp8(desc, &need);
+    if (q != MOE_OK) return q;
+    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    int st = moe_route_topk(desc, x, w_router, bias, 0, logits, scores, topk_idx, topk_score, workspace, workspace_bytes, stream);
+    if (st != MOE_OK) return st;
+    // the last launch of the drop builds the tile schedule of the products, behind what the drop itself uses
+    const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, drop_workspace(*desc, s, nullptr).bytes, workspace);
+    const int hp = fp8_pitch(desc->d_hidden);
+    const Fp8Gemm down = fp8_gemm(desc->n_experts, s.max_rows, hp, desc->d_model);
+    const FfnScheduleArgs schedule =
+        schedule_args(ws.f, fp8_gemm(desc->n_experts, s.max_rows, desc->d_model, hp), true, &down, compute_units());
+    st = capacity_drop_impl(desc, scores, topk_idx, token_class, seed, expert_count, seg_count, expert_offset, row_token,
+                            row_weight, pair_row, workspace, workspace_bytes, s.max_rows > 0 ? &schedule : nullptr, stream);
+    if (st != MOE_OK) return st;
+    if (s.max_rows > 0) {
+        st = ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, true, stream);
+        if (st != MOE_OK) return st;
+    }
+    return moe_combine(desc, yp, row_weight, pair_row, y, stream);
+}
+
+}  // extern "C"

@@ -25,6 +25,10 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 __global__ __launch_bounds__(64) void ffn_schedule_kernel(const int32_t* __restrict__ expert_offset, FfnScheduleArgs args) {
     build_ffn_schedule(expert_offset, args);
 }
+void launch_ffn_schedule(const int32_t* expert_offset, const FfnScheduleArgs& args, hipStream_t st) {
+    ProfileScope prof(MOE_KERNEL_FFN_SCHEDULE, st);
+    hipLaunchKernelGGL(ffn_schedule_kernel, dim3(1), dim3(64), 0, st, expert_offset, args);
+}
 
 // ---------------------------------------------------------------------------------------------
 // tiles on 16x16x32 matrix instructions, four waves
@@ -375,20 +379,6 @@ __global__ __launch_bounds__(S::kThreads) void ffn_gemm_bf16_kernel(
     }
 }
 
-// The three tile lists of a workspace as the kernels take them; joint == false leaves the joint list unwritten
-// (the fp32 kernels walk the list of big tiles only).
-static TileListArgs tile_list_args(const FfnWorkspace& ws, bool joint) {
-    return TileListArgs{ws.big.expert, ws.big.row0,  ws.big.rows,      ws.big.count,       ws.small.expert,
-                        ws.small.row0, ws.small.rows, ws.small.count,   ws.big.max_tiles,   ws.small.max_tiles,
-                        ws.all.expert, ws.all.row0,  ws.all.rows,      ws.all.count,       joint ? ws.all.max_tiles : 0};
-}
-
-static int column_group(int nb_total) {
-    for (int g = 4; g > 1; --g)
-        if (nb_total % g == 0) return g;
-    return 1;
-}
-
 template <int BN, bool SWIGLU>
 static void launch_bf16(bool stream, const void* A, const void* B0, const void* B1, void* C, const int32_t* gather,
                         const FfnWorkspace& ws, int K, int Nout, const int32_t* split_hdr, int32_t* split_counter,
@@ -483,10 +473,7 @@ hipError_t launch_grouped_ffn(const moe_desc_t& d, const Sizes& s, const FfnWork
     const int K1 = d.d_model, N1 = d.d_hidden, K2 = d.d_hidden, N2 = d.d_model;
     const bool bf16 = d.dtype == MOE_DTYPE_BF16;
     const int bn_down = N2 % 256 == 0 ? 256 : 128;  // d is a multiple of 128 at least: output columns per block
-    if (!schedule_ready) {
-        ProfileScope prof(MOE_KERNEL_FFN_SCHEDULE, st);
-        hipLaunchKernelGGL(ffn_schedule_kernel, dim3(1), dim3(64), 0, st, expert_offset, ffn_schedule_args(d, ws, compute_units()));
-    }
+    if (!schedule_ready) launch_ffn_schedule(expert_offset, ffn_schedule_args(d, ws, compute_units()), st);
     if (ffn_is_thin(d, s)) {
         launch_ffn_thin(d, s, ws, xp, row_token, w_gate, w_up, w_down, yp, st);
     } else if (bf16) {

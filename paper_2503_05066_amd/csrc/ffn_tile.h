@@ -490,4 +490,18 @@ __device__ __forceinline__ void wait_for_all_but(int n) {
 // the short items: at most kFfnSplitUnits / 8 - 1 items of an XCD are cut (what is left after full rounds).
 constexpr int kXcdTicket = kFfnSplitUnits / 8 - 1, kPoolTicket = kFfnSplitUnits + kFfnSplitUnits / 8 - 1;
 
+// The three tile lists of a workspace as the kernels take them; joint == false leaves the joint list unwritten
+// (the fp32 kernels walk the list of big tiles only).
+inline TileListArgs tile_list_args(const FfnWorkspace& ws, bool joint) {
+    return TileListArgs{ws.big.expert, ws.big.row0,  ws.big.rows,      ws.big.count,       ws.small.expert,
+                        ws.small.row0, ws.small.rows, ws.small.count,   ws.big.max_tiles,   ws.small.max_tiles,
+                        ws.all.expert, ws.all.row0,  ws.all.rows,      ws.all.count,       joint ? ws.all.max_tiles : 0};
+}
+
+inline int column_group(int nb_total) {
+    for (int g = 4; g > 1; --g)
+        if (nb_total % g == 0) return g;
+    return 1;
+}
+
 }  // namespace capmoe

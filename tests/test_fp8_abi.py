@@ -1,0 +1,187 @@
+"""The 8-bit experts without a GPU: sizes, refusals before anything is launched, and the reference's own format."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import fp8_reference as ref
+from paper_2503_05066_amd import capmoe
+
+pytestmark = pytest.mark.usefixtures("built_library")
+OK, INVALID, UNSUPPORTED, SMALL = 0, 1, 2, 3
+P = 1 << 20  # an aligned address that nothing reads
+
+
+def test_reference_values_are_those_of_the_type():
+    bytes_ = torch.arange(256, dtype=torch.uint8)
+    want = bytes_.view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(ref.E4M3, want, equal_nan=True)
+    v = np.concatenate([np.random.default_rng(1).uniform(-448, 448, 20000), ref.E4M3[:126], (ref.E4M3[:126] + ref.E4M3[1:127]) / 2])
+    got = ref.encode(np.float64(np.float32(v)))
+    want = torch.from_numpy(np.float32(v)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("amax,byte", [(448.0, 127), (448.0001, 128), (1.75, 119), (1.75001, 120), (0.0, 0), (1e-45, 0),
+                                       (3.4e38, 247), (448.0 * 2.0 ** -127, 0), (449.0 * 2.0 ** -127, 1)])
+def test_reference_scales(amax, byte):
+    assert ref.block_byte(np.array([amax]))[0] == byte
+
+
+@pytest.mark.parametrize("cols,pitch,scale", [(1, 128, 4), (128, 128, 4), (129, 256, 4), (512, 512, 4), (520, 640, 8),
+                                              (14336, 14336, 112), (1 << 21, 1 << 21, 1 << 14)])
+def test_sizes(cols, pitch, scale):
+    assert capmoe.moe_fp8_query(cols) == (pitch, scale)
+
+
+def test_size_refusals():
+    lib = capmoe.load()
+    assert lib.moe_fp8_query(0, None, None) == INVALID
+    assert lib.moe_fp8_query((1 << 21) + 1, None, None) == UNSUPPORTED
+
+
+def test_quantize_rows_refusals():
+    f = capmoe.load().moe_quantize_rows
+    good = dict(dtype=1, x=P, n=4, cols=64, token=None, count=None, q=P, s=P)
+
+    def call(**change):
+        a = {**good, **change}
+        return f(a["dtype"], a["x"], a["n"], a["cols"], a["token"], a["count"], a["q"], a["s"], None)
+
+    assert call(dtype=2) == INVALID and call(dtype=-1) == INVALID
+    assert call(n=-1) == INVALID and call(cols=0) == INVALID and call(cols=-8) == INVALID
+    assert call(cols=12) == UNSUPPORTED and call(dtype=0, cols=6) == UNSUPPORTED
+    assert call(cols=(1 << 21) + 8) == UNSUPPORTED
+    assert call(n=1 << 31) == UNSUPPORTED and call(n=1 << 30, cols=256) == UNSUPPORTED and call(n=1 << 62, cols=1 << 20) == UNSUPPORTED
+    for a in ("x", "q", "s"):
+        assert call(**{a: None}) == INVALID
+    assert call(x=P + 8) == INVALID and call(q=P + 8) == INVALID and call(s=P + 2) == INVALID
+    assert call(n=0, x=None, q=None, s=None) == OK
+
+
+def test_quantize_weights_refusals():
+    f = capmoe.load().moe_quantize_weights
+    good = dict(dtype=1, w=P, e=2, n=16, k=64, q=P, s=P)
+
+    def call(**change):
+        a = {**good, **change}
+        return f(a["dtype"], a["w"], a["e"], a["n"], a["k"], a["q"], a["s"], None)
+
+    assert call(dtype=7) == INVALID and call(e=0) == INVALID and call(n=0) == INVALID and call(k=0) == INVALID
+    assert call(k=12) == UNSUPPORTED and call(dtype=0, k=3) == UNSUPPORTED and call(n=(1 << 21) + 1) == UNSUPPORTED
+    assert call(e=1 << 10, n=1 << 21, k=1 << 21) == UNSUPPORTED
+    for a in ("w", "q", "s"):
+        assert call(**{a: None}) == INVALID
+    assert call(w=P + 4) == INVALID and call(q=P + 1) == INVALID and call(s=P + 1) == INVALID
+
+
+def test_gemm_refusals():
+    lib = capmoe.load()
+    good = dict(rows=8, src=0, e=4, k=256, n=64, x=P, xs=P, token=None, off=P, w=P, ws=P, y=P, work=P, size=1 << 30)
+
+    def call(**change):
+        a = {**good, **change}
+        g = capmoe.MoeGemm(a["rows"], a["src"], a["e"], a["k"], a["n"])
+        return lib.moe_grouped_gemm_fp8(ctypes.byref(g), a["x"], a["xs"], a["token"], a["off"], a["w"], a["ws"], a["y"],
+                                        a["work"], a["size"], None)
+
+    for bad in (dict(rows=-1), dict(src=-1), dict(e=0), dict(k=0), dict(n=0)):
+        assert call(**bad) == INVALID
+    for bad in (dict(e=257), dict(n=12), dict(n=(1 << 21) + 8), dict(k=(1 << 21) + 1), dict(token=P, src=1 << 20, k=1 << 13)):
+        assert call(**bad) == UNSUPPORTED
+    for a in ("x", "xs", "off", "w", "ws", "y", "work"):
+        assert call(**{a: None}) == INVALID
+    for a in ("x", "w", "y"):
+        assert call(**{a: P + 8}) == INVALID
+    assert call(xs=P + 2) == INVALID and call(ws=P + 1) == INVALID and call(work=P + 128) == INVALID
+    need = capmoe.moe_gemm_query(capmoe.make_gemm(8, 256, 64, 4))
+    assert call(size=need - 1) == SMALL
+    assert call(rows=0) == OK  # nothing to do, nothing launched
+    assert lib.moe_grouped_gemm_fp8(None, P, P, None, P, P, P, P, P, 1 << 30, None) == INVALID
+    assert lib.moe_gemm_query(None, None) == INVALID
+
+
+def _desc(**more):
+    a = dict(n_tokens=16, d_model=256, n_experts=8, top_k=2, d_hidden=200, dtype=capmoe.DTYPE_BF16)
+    a.update(more)
+    return capmoe.make_desc(**a)
+
+
+def _experts(**change):
+    e = capmoe.MoeFp8Experts(P, P, P, P, P, P)
+    for k, v in change.items():
+        setattr(e, k, v)
+    return e
+
+
+def test_ffn_refusals():
+    lib = capmoe.load()
+
+    def grouped(desc=None, x=P, off=P, experts=None, yp=P, work=P, size=1 << 40):
+        return lib.moe_grouped_ffn_fp8(ctypes.byref(desc or _desc()), x, off, ctypes.byref(experts or _experts()), yp, work, size, None)
+
+    def fused(desc=None, x=P, off=P, token=P, experts=None, yp=P, work=P, size=1 << 40):
+        return lib.moe_dispatch_ffn_fp8(ctypes.byref(desc or _desc()), x, off, token, ctypes.byref(experts or _experts()), yp, work, size, None)
+
+    for f in (grouped, fused):
+        assert f(desc=_desc(dtype=capmoe.DTYPE_F32)) == UNSUPPORTED
+        assert f(desc=_desc(d_hidden=(1 << 21) + 1)) == UNSUPPORTED
+        assert f(desc=_desc(d_model=252)) == UNSUPPORTED  # no 16-byte pieces
+        assert f(desc=_desc(top_k=9)) == INVALID
+        for a in ("x", "off", "yp", "work"):
+            assert f(**{a: None}) == INVALID
+        assert f(x=P + 8) == INVALID and f(yp=P + 8) == INVALID and f(work=P + 8) == INVALID
+        for name, _ in capmoe.MoeFp8Experts._fields_:
+            assert f(experts=_experts(**{name: None})) == INVALID
+            assert f(experts=_experts(**{name: P + 2})) == INVALID
+        assert f(size=1024) == SMALL
+        assert f(desc=_desc(gamma=0.0)) == OK  # no row can survive
+    assert fused(token=None) == INVALID
+    assert fused(desc=_desc(n_tokens=1 << 17, d_model=1 << 14)) == UNSUPPORTED
+    assert lib.moe_grouped_ffn_fp8(ctypes.byref(_desc()), P, P, None, P, P, 1 << 40, None) == INVALID
+
+
+def test_layer_refusals():
+    lib = capmoe.load()
+    names = ("logits", "scores", "topk_idx", "topk_score", "expert_count", "seg_count", "expert_offset", "row_token",
+             "row_weight", "pair_row", "yp", "y", "workspace")
+
+    def call(desc=None, x=P, w_router=P, experts=None, size=1 << 40, **change):
+        a = {**{n: P for n in names}, **change}
+        return lib.moe_layer_forward_fp8(ctypes.byref(desc or _desc()), x, w_router, None, ctypes.byref(experts or _experts()), None, 0,
+                                         *[a[n] for n in names], size, None)
+
+    assert call(desc=_desc(dtype=capmoe.DTYPE_F32)) == UNSUPPORTED
+    assert call(x=None) == INVALID and call(w_router=None) == INVALID and call(x=P + 8) == INVALID
+    for n in names:
+        assert call(**{n: None}) == INVALID, n
+    for n in ("scores", "topk_idx", "pair_row", "yp", "y", "workspace"):
+        assert call(**{n: P + 4}) == INVALID, n
+    assert call(experts=_experts(down=None)) == INVALID
+    need = capmoe.moe_query_fp8(_desc())
+    assert call(size=need - 1) == SMALL and need >= capmoe.moe_query(_desc())[3]
+
+
+def test_query_refuses_other_types():
+    with pytest.raises(capmoe.CapMoeError) as e:
+        capmoe.moe_query_fp8(_desc(dtype=capmoe.DTYPE_F32))
+    assert e.value.status == UNSUPPORTED
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    x = torch.zeros((4, 64), dtype=torch.bfloat16)
+    q, s = capmoe.fp8_row_buffers(4, 64, device="cpu")
+    for bad in (lambda: capmoe.moe_quantize_rows(x, None, None, q[:, :64], s), lambda: capmoe.moe_quantize_rows(x, None, None, q, s[:2]),
+                lambda: capmoe.moe_quantize_rows(x, None, None, torch.cat([q, q]), torch.cat([s, s])),
+                lambda: capmoe.moe_quantize_rows(x.half(), None, None, q, s), lambda: capmoe.moe_quantize_rows(x.T, None, None, q, s),
+                lambda: capmoe.moe_quantize_rows(x, torch.zeros(3, dtype=torch.int32), None, q, s),
+                lambda: capmoe.moe_quantize_rows(x, torch.zeros(4, dtype=torch.int64), None, q, s)):
+        with pytest.raises(ValueError):
+            bad()
+    w = torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+    q, s = capmoe.fp8_weight_buffers(2, 8, 64, device="cpu")
+    for bad in (lambda: capmoe.moe_quantize_weights(w, q[:, :8], s), lambda: capmoe.moe_quantize_weights(w, q, s[:1]),
+                lambda: capmoe.moe_quantize_weights(w.transpose(0, 1), q, s), lambda: capmoe.moe_quantize_weights(w[0], q, s)):
+        with pytest.raises(ValueError):
+            bad()

@@ -1,0 +1,339 @@
+"""The 8-bit experts on the GPU against the formulas in 64 bits.
+
+Quantising is exact: the same bytes.  A product's result differs from the 64-bit sum by its one rounding to bf16, at most
+2^-8 of the value, and by what the matrix cores' fp32 sums lose: the 8-bit instructions add the products of a few k with
+their bits aligned to the largest one, which costs up to 2^-12 of the sum of their magnitudes (2^-13.4 on bytes drawn
+evenly from the whole type).  In the FFN a hidden value that lies that close to a border between two 8-bit values may fall
+on the other side: 2^-13 against steps of 2^-3 is one value in 2^10, off by 2^-4 to 2^-3, which adds at most
+2^-3 * 2^-5 = 2^-8 to the 2-norm; with the two roundings to bf16 less than 2^-7.
+"""
+import numpy as np
+import pytest
+import torch
+
+import fp8_reference as ref
+from paper_2503_05066_amd import capmoe
+
+pytestmark = [pytest.mark.gpu, pytest.mark.usefixtures("built_library")]
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _device():
+    torch.cuda.set_device(0)
+
+
+def rng(*key):
+    return np.random.default_rng(list(key))
+
+
+def on(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def plain(t):
+    return t.double().cpu().numpy()
+
+
+def awkward(g, r, c):
+    """Values of many sizes with rows of zeros, the type's ends, exact ties and numbers that are not finite."""
+    x = g.standard_normal((r, c)) * np.exp(3 * g.standard_normal((r, 1)))
+    x[0] = 0
+    for i, f in enumerate((lambda v: v * 2.0 ** -125, lambda v: v * 2.0 ** -132, lambda v: np.where(v > 0, 3.3e38, -3.0e38),
+                           lambda v: 448.0 * np.sign(v), lambda v: np.where(v > 1, 2.0, 1.5), lambda v: -0.0 * np.ones(c))):
+        if r > 1 + i:
+            x[1 + i] = f(g.standard_normal(c))
+    if r > 8:
+        x[7, :: max(1, c // 3)] = np.nan
+        x[8, 0], x[8, c - 1] = np.inf, -np.inf
+    return x
+
+
+ROWS = [(1, 8), (1, 64), (3, 72), (37, 4096), (9, 128), (11, 136), (64, 1416), (5, 520), (130, 2048), (2, 14336)]
+
+
+@pytest.mark.parametrize("rows,cols", ROWS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_have_the_bytes_of_the_definition(rows, cols, dtype):
+    x = on(awkward(rng(rows, cols), rows, cols), dtype)
+    q, s = capmoe.fp8_row_buffers(rows, cols)
+    q.fill_(0x55), s.fill_(0x55)
+    capmoe.moe_quantize_rows(x, None, None, q, s)
+    want_q, want_s = ref.quantize_rows(plain(x))
+    assert np.array_equal(s.cpu().numpy(), want_s)
+    got = q.cpu().numpy()
+    nan = (want_q & 127) == 127
+    assert np.array_equal(np.where(nan, 0, got), np.where(nan, 0, want_q)) and np.all(got[nan] & 127 == 127)
+
+
+def test_rows_narrower_than_a_block_of_fp32():
+    x = on(rng(4).standard_normal((5, 4)), F32)
+    q, s = capmoe.fp8_row_buffers(5, 4)
+    capmoe.moe_quantize_rows(x, None, None, q, s)
+    want_q, want_s = ref.quantize_rows(plain(x))
+    assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(s.cpu().numpy(), want_s)
+
+
+@pytest.mark.parametrize("count", [-3, 0, 1, 40, 64, 1000])
+def test_rows_are_permuted_and_those_behind_the_count_untouched(count):
+    g = rng(7)
+    x = on(g.standard_normal((20, 264)), BF16)
+    token = g.integers(0, 20, 64).astype(np.int32)
+    token[:4] = 19, 19, 0, 0
+    q, s = capmoe.fp8_row_buffers(64, 264)
+    q.fill_(0x33), s.fill_(0x33)
+    capmoe.moe_quantize_rows(x, on(token), on(np.array([count], np.int32)), q, s)
+    want_q, want_s = ref.quantize_rows(plain(x)[token])
+    n = min(max(count, 0), 64)
+    got_q, got_s = q.cpu().numpy(), s.cpu().numpy()
+    assert np.array_equal(got_q[:n], want_q[:n]) and np.array_equal(got_s[:n], want_s[:n])
+    assert np.all(got_q[n:] == 0x33) and np.all(got_s[n:] == 0x33)
+
+
+@pytest.mark.parametrize("e,n,k", [(1, 1, 8), (3, 130, 136), (2, 1000, 1416), (1, 128, 128), (5, 24, 520), (2, 256, 2048)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weights_have_the_bytes_of_the_definition(e, n, k, dtype):
+    w = rng(e, n, k).standard_normal((e, n, k))
+    if n > 100:
+        w[0, 1, 3], w[0, 2, 4] = np.nan, np.inf
+        w[-1, :128, :128] = 0
+        w[-1, -2:] *= 1e30
+    w = on(w, dtype)
+    q, s = capmoe.fp8_weight_buffers(e, n, k)
+    q.fill_(0x55), s.fill_(0x55)
+    capmoe.moe_quantize_weights(w, q, s)
+    want_q, want_s = ref.quantize_weights(plain(w))
+    got = q.cpu().numpy()
+    nan = (want_q & 127) == 127
+    assert np.array_equal(s.cpu().numpy(), want_s)
+    assert np.array_equal(np.where(nan, 0, got), np.where(nan, 0, want_q)) and np.all(got[nan] & 127 == 127)
+
+
+class Product:
+    """8-bit rows and weights of the given sizes, on the device and as 64-bit values."""
+
+    def __init__(self, counts, k, n, src=0, seed=0, scale_spread=0.0):
+        g = rng(seed, len(counts), k, n)
+        self.offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        self.rows, self.e, self.k, self.n = int(self.offset[-1]), len(counts), k, n
+        r = src or max(self.rows, 1)
+        x = g.standard_normal((r, k)) * np.exp(scale_spread * g.standard_normal((r, k)))
+        w = g.standard_normal((self.e, n, k)) * k ** -0.5 * np.exp(scale_spread * g.standard_normal((self.e, n, k)))
+        self.xq, self.xs = ref.quantize_rows(x)
+        self.wq, self.ws = ref.quantize_weights(w)
+        self.token = g.integers(0, r, max(self.rows, 1)).astype(np.int32) if src else None
+        self.src = src
+
+    def run(self, extra=0, workspace=None):
+        g = capmoe.make_gemm(self.rows + extra, self.k, self.n, self.e, src_rows=self.src)
+        y = torch.full((self.rows + extra, self.n), 7.0, dtype=BF16, device="cuda")
+        self.keep = [on(a) for a in (self.xq, self.xs, self.offset, self.wq, self.ws)]
+        token = None if self.token is None else on(np.concatenate([self.token, np.zeros(extra, np.int32)]))
+        ws = torch.empty(capmoe.moe_gemm_query(g), dtype=torch.uint8, device="cuda")
+        ws.fill_(0xA5)
+        x, xs, off, w, wsc = self.keep
+        capmoe.moe_grouped_gemm_fp8(g, x, xs, token, off, w, wsc, y, ws)
+        torch.cuda.synchronize()
+        return y
+
+    def check(self, y):
+        want, mag = ref.gemm(ref.rows_value(self.xq, self.xs), ref.weights_value(self.wq, self.ws), self.offset, self.token)
+        want, mag = want[:, : self.n], mag[:, : self.n]
+        got = plain(y)[: self.rows]
+        off = np.abs(got - want)
+        assert np.all(off <= 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * mag), np.max(off / (2.0 ** -8 * np.abs(want) + 2.0 ** -12 * mag))
+        assert np.linalg.norm(off) <= 2.0 ** -8 * np.linalg.norm(want)
+
+
+COUNTS = {"one": [1], "none": [0, 0, 0], "holes": [0, 1, 0, 17, 0], "sixteens": [16, 15, 33, 32], "tiles": [64, 65, 256, 255],
+          "high": [257, 300, 0, 513], "ragged": [129, 3, 0, 160, 95, 224, 31, 200]}
+
+
+@pytest.mark.parametrize("counts", COUNTS)
+@pytest.mark.parametrize("k,n", [(128, 128), (8, 8), (520, 264), (256, 1000), (1416, 128), (2048, 256)])
+def test_product(counts, k, n):
+    p = Product(COUNTS[counts], k, n)
+    y = p.run(extra=5)
+    assert torch.all(y[p.rows:] == 7.0)  # rows behind the last expert's
+    p.check(y)
+
+
+@pytest.mark.parametrize("counts,k,n", [([40, 0, 300, 7], 520, 264), ([1, 1, 1], 2048, 1024), ([600], 384, 512)])
+def test_product_through_a_plan(counts, k, n):
+    p = Product(counts, k, n, src=50)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("counts,k,n", [([700, 20], 640, 256), ([9, 30], 1024, 136)])
+def test_product_of_values_of_many_sizes(counts, k, n):
+    p = Product(counts, k, n, scale_spread=2.0)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("counts", [[300], [5, 12]])
+def test_every_block_has_its_own_scale(counts):
+    # ones everywhere, scales alone differ: a scale taken from another row, column block or k block shows as a power of two
+    p = Product(counts, 1416, 392)
+    g = rng(3)
+    kb = 12
+    p.xq[:], p.wq[:] = 0x38, 0x38  # e4m3 of 1
+    p.xs[:, :kb] = g.integers(120, 134, p.xs[:, :kb].shape)
+    p.ws[:, :, :kb] = g.integers(120, 134, p.ws[:, :, :kb].shape)
+    p.check(p.run())
+
+
+def test_nan_and_zero_rows_stay_by_themselves():
+    p = Product([40, 300], 512, 256)
+    p.xq[3, 100] = 0x7F
+    p.xq[50, 511] = 0xFF
+    p.xq[51] = 0
+    got = plain(p.run())
+    assert np.all(np.isnan(got[[3, 50]])) and np.all(got[51] == 0)
+    rest = np.delete(np.arange(340), [3, 50])
+    assert np.all(np.isfinite(got[rest]))
+
+
+def layer(tokens, d, e, k, h, seed=0, **more):
+    g = rng(seed, tokens, d, e, h)
+    desc = capmoe.make_desc(tokens, d, e, k, h, **more)
+    x = on(g.standard_normal((tokens, d)), BF16)
+    weights = [on(g.standard_normal(s) * s[2] ** -0.5, BF16) for s in ((e, h, d), (e, h, d), (e, d, h))]
+    return desc, x, weights, on(g.standard_normal((e, d)) * d ** -0.5, F32), on(g.standard_normal(e), F32)
+
+
+def plan_of(g, tokens, counts):
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    token = np.concatenate([np.sort(g.choice(tokens, c, replace=False)) for c in counts] + [np.zeros(0)]).astype(np.int32)
+    return offset, token
+
+
+FFN = [(1, 256, 8, 2, 128, [1, 0, 0, 0, 0, 0, 0, 1]), (16, 512, 4, 2, 384, [16, 0, 7, 9]), (37, 264, 6, 2, 200, [37, 1, 0, 20, 16, 0]),
+       (300, 256, 4, 2, 384, [300, 2, 0, 290]), (520, 1032, 3, 2, 136, [520, 64, 300]), (700, 384, 5, 2, 1416, [257, 700, 100, 0, 33]),
+       (5, 136, 2, 1, 8, [2, 3]), (1000, 512, 8, 4, 640, [1000, 700, 512, 256, 255, 96, 0, 130])]
+
+
+@pytest.mark.parametrize("tokens,d,e,k,h,counts", FFN)
+def test_ffn(tokens, d, e, k, h, counts):
+    desc, x, weights, _, _ = layer(tokens, d, e, k, h, mode=capmoe.MODE_NONE)
+    offset, token = plan_of(rng(1, tokens), tokens, counts)
+    rows = len(token)
+    assert rows <= tokens * k or tokens < 10
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    max_rows = capmoe.moe_query(desc)[2]
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xA5)
+    yp = torch.full((max_rows + 3, d), 7.0, dtype=BF16, device="cuda")
+    padded = np.zeros(max_rows, np.int32)
+    padded[:rows] = token
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(padded), experts, yp, ws)
+    got = plain(yp)
+    assert np.all(got[rows:] == 7.0)
+    values = [ref.weights_value(*ref.quantize_weights(plain(w))) for w in weights]
+    want = ref.ffn(plain(x), *values, offset, token)[:, :d]
+    off = got[:rows] - want
+    assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want), np.linalg.norm(off) / np.linalg.norm(want)
+    rms = np.sqrt(np.mean(want ** 2))
+    assert np.abs(off).max() <= 0.5 * np.maximum(rms, np.abs(want).max() / 8)
+    # the two calls on permuted rows: the same bits
+    xp = torch.zeros((max_rows, d), dtype=BF16, device="cuda")
+    capmoe.moe_dispatch(desc, x, on(offset), on(padded), xp)
+    yp2 = torch.full_like(yp, 7.0)
+    ws.fill_(0x5A)
+    capmoe.moe_grouped_ffn_fp8(desc, xp, on(offset), experts, yp2, ws)
+    assert torch.equal(yp, yp2)
+
+
+def test_a_token_that_is_not_a_number_stays_by_itself():
+    desc, x, weights, _, _ = layer(400, 256, 4, 1, 384, mode=capmoe.MODE_NONE)
+    x[7, 3], x[200, 255] = float("nan"), float("inf")
+    counts = [300, 12, 0, 88]
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    token = np.arange(400, dtype=np.int32)
+    token[[7, 305]] = 305, 7  # one among the long expert's rows, one among the short one's
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    yp = torch.zeros((400, 256), dtype=BF16, device="cuda")
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(token), experts, yp, ws)
+    bad = np.isnan(plain(yp)).any(axis=1)
+    assert set(np.flatnonzero(bad)) == {200, 305}
+
+
+LAYERS = [dict(tokens=64, d=256, e=8, k=2, h=384, device_groups=4, mode=capmoe.MODE_EXPANDED_DROP),
+          dict(tokens=512, d=512, e=16, k=4, h=640, mode=capmoe.MODE_TOKEN_DROP, gamma=1.5),
+          dict(tokens=1, d=264, e=8, k=2, h=200, mode=capmoe.MODE_NONE),
+          dict(tokens=300, d=256, e=4, k=1, h=128, mode=capmoe.MODE_TOKEN_DROP, gamma=0.0),
+          dict(tokens=2048, d=256, e=8, k=2, h=256, mode=capmoe.MODE_TOKEN_DROP, capacity_scope=capmoe.SCOPE_GLOBAL)]
+
+
+def separate(desc, x, w_router, bias, experts):
+    buf = capmoe.LayerBuffers(desc, fp8=True)
+    capmoe.moe_route_topk(desc, x, w_router, bias, 0, buf.logits, buf.scores, buf.topk_idx, buf.topk_score, buf.workspace)
+    capmoe.moe_capacity_drop(desc, buf.scores, buf.topk_idx, buf.expert_count, buf.seg_count, buf.expert_offset, buf.row_token,
+                             buf.row_weight, buf.pair_row, buf.workspace)
+    capmoe.moe_dispatch_ffn_fp8(desc, x, buf.expert_offset, buf.row_token, experts, buf.yp, buf.workspace)
+    capmoe.moe_combine(desc, buf.yp, buf.row_weight, buf.pair_row, buf.y)
+    return buf
+
+
+@pytest.mark.parametrize("case", range(len(LAYERS)))
+def test_layer_is_the_separate_calls(case):
+    desc, x, weights, w_router, bias = layer(**LAYERS[case])
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    want = separate(desc, x, w_router, bias, experts)
+    got = capmoe.LayerBuffers(desc, fp8=True)
+    got.workspace.fill_(0xA5)
+    capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, experts, None, 0, got)
+    rows = int(want.expert_offset[-1])
+    assert torch.equal(got.expert_offset, want.expert_offset) and torch.equal(got.pair_row, want.pair_row)
+    assert torch.equal(got.yp[:rows], want.yp[:rows]) and torch.equal(got.y, want.y)
+    # and close to the same layer in bf16: the values are off by 2^-4 at most, 2^-5.6 in the mean square, in three products' operands
+    buf = capmoe.LayerBuffers(desc)
+    if desc.d_model % 128 == 0 and desc.d_hidden % 128 == 0 and rows:
+        y = capmoe.moe_layer_forward(desc, x, w_router, bias, *weights, None, 0, buf)
+        assert float((y.float() - got.y.float()).norm() / y.float().norm()) < 0.1
+
+
+def test_captured_layer_replays():
+    desc, x, weights, w_router, bias = layer(**LAYERS[1])
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    buf = capmoe.LayerBuffers(desc, fp8=True)
+    capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, experts, None, 0, buf)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, experts, None, 0, buf)
+    for i in range(4):
+        x.copy_(on(rng(50 + i).standard_normal(tuple(x.shape)), BF16))
+        graph.replay()
+        got = buf.y.clone()
+        want = capmoe.LayerBuffers(desc, fp8=True)
+        capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, experts, None, 0, want)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want.y), i
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    p, r = Product([300, 20, 0, 64], 512, 384, seed=1), Product([5, 9, 1, 0], 640, 264, seed=2)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    out = []
+    inputs = []
+    for q in (p, r):
+        g = capmoe.make_gemm(q.rows, q.k, q.n, q.e)
+        inputs.append((g, [on(a) for a in (q.xq, q.xs, q.offset, q.wq, q.ws)], torch.zeros((q.rows, q.n), dtype=BF16, device="cuda"),
+                       torch.empty(capmoe.moe_gemm_query(g), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, (g, (x, xs, off, w, ws), y, work) in zip(streams, inputs):
+            capmoe.moe_grouped_gemm_fp8(g, x, xs, None, off, w, ws, y, work, stream=st)
+    torch.cuda.synchronize()
+    for q, (_, _, y, _) in zip((p, r), inputs):
+        q.check(y)
+
+
+def test_the_same_call_gives_the_same_bits():
+    p = Product([700, 40, 0, 300, 1], 2048, 1024, seed=5)
+    first = p.run()
+    for _ in range(3):
+        assert torch.equal(first, p.run())
