@@ -20,7 +20,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libcapmoe.so")
 
 SOURCES = ["api.hip", "route.hip", "router_mfma.hip", "drop.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip", "probe.hip",
-           "quantize.hip", "fp8_thin.hip", "api_fp8.hip"]
+           "quantize.hip", "fp8.hip", "fp8_thin.hip", "api_fp8.hip"]
 # the packed-fp32 feature is switched off for all device code; the first sixteen words of a kernel's arguments arrive in
 # registers (a token through 64 experts x 2048 x 1024: 38.3 -> 37.7 us); the router file must not contract
 # multiplies and adds (its softmax is a fixed sequence of individually rounded operations)
@@ -29,7 +29,9 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", os.path.j
           "-Wno-unused-command-line-argument"]
 PER_FILE = {"route.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"]}
 # sources whose asm statements name accumulation registers: the assembly of the same compilation is checked
-NAMED_ACCUMULATORS = {"ffn.hip"}
+NAMED_ACCUMULATORS = {"ffn.hip", "fp8.hip"}
+# a source that is compiled in parts, an object each
+PARTS = {"fp8.hip": [["-DCAPMOE_FP8_SHAPE=%d" % i] for i in range(3)]}
 
 
 def _hipcc() -> str:
@@ -59,13 +61,17 @@ def compile_source(source: str, obj: str, flags=(), named_accumulators: bool = F
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
 
-    def compile_one(src):
-        obj = os.path.join(OBJ, src.replace(".hip", ".o"))
-        compile_source(os.path.join(CSRC, src), obj, PER_FILE.get(src, []), src in NAMED_ACCUMULATORS, verbose)
+    def compile_one(job):
+        src, part, flags = job
+        obj = os.path.join(OBJ, src.replace(".hip", "%s.o" % part))
+        compile_source(os.path.join(CSRC, src), obj, PER_FILE.get(src, []) + flags, src in NAMED_ACCUMULATORS, verbose)
         return obj
 
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        objs = list(ex.map(compile_one, SOURCES))
+    jobs = [(src, "_%d" % i if len(parts) > 1 else "", flags) for src in SOURCES
+            for parts in [PARTS.get(src, [[]])] for i, flags in enumerate(parts)]
+    jobs.sort(key=lambda job: job[0] not in PARTS)  # the longest first
+    with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
+        objs = list(ex.map(compile_one, jobs))
     r = subprocess.run([_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs],
                        capture_output=True, text=True)
     if r.returncode != 0:

@@ -8,7 +8,8 @@ namespace capmoe {
 
 // Workspace of a layer's FFN, or of one product (h == 0: no quantised x, no hidden activation).
 struct Fp8Workspace {
-    FfnWorkspace f;         // hidden: [P_max, h filled up] bf16
+    FfnWorkspace f;         // hidden: [P_max, h filled up] bf16, or 8-bit values and behind them their scales
+    uint8_t* hidden_scale;
     void* xq;               // [rows of x, pitch]
     uint8_t* xs;
     size_t bytes;
@@ -17,7 +18,7 @@ struct Fp8Workspace {
 static Fp8Workspace gemm_workspace(const Fp8Gemm& g, void* base) {
     Fp8Workspace w;
     size_t off = 0;
-    w.f.hidden = nullptr, w.xq = nullptr, w.xs = nullptr;
+    w.f.hidden = nullptr, w.hidden_scale = nullptr, w.xq = nullptr, w.xs = nullptr;
     place_schedule(w.f, (char*)base, off, g.experts, g.max_rows, true, false);
     w.bytes = off;
     return w;
@@ -30,7 +31,9 @@ static Fp8Workspace ffn_fp8_workspace(const moe_desc_t& d, const Sizes& s, size_
     size_t off = 0;
     const int64_t rows = std::max<int64_t>(s.max_rows, 1);
     w.f.hidden = p + off;
-    off += align256((size_t)rows * fp8_pitch(d.d_hidden) * 2);
+    w.hidden_scale = (uint8_t*)(p + off + align256((size_t)rows * fp8_pitch(d.d_hidden)));
+    off += align256((size_t)rows * fp8_pitch(d.d_hidden)) + align256((size_t)rows * fp8_pitch(d.d_hidden));
+    static_assert(kFp8Block >= 4, "a row's scale bytes fit where its second byte per value would be");
     const int64_t x_rows = std::max<int64_t>(rows, d.n_tokens);
     w.xq = p + off;
     off += align256((size_t)x_rows * fp8_pitch(d.d_model));
@@ -90,6 +93,37 @@ static int validate_experts(const moe_fp8_experts_t* w) {
 
 static bool weights_stream(double bytes) { return bytes > (double)(320ull << 20); }
 
+// One product on the tiles of a schedule (fp8.hip).  which: 0 or 1, its header in the schedule.
+static void launch_fp8_tiles(const Fp8Gemm& g, const FfnWorkspace& ws, int which, const void* x, const uint8_t* x_scale,
+                             const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up,
+                             const uint8_t* up_scale, void* y, uint8_t* y_scale, bool stream, hipStream_t st) {
+    Fp8Args p;
+    p.x = (const uint8_t*)x, p.x_scale = x_scale, p.gather = gather;
+    p.w[0] = (const uint8_t*)w, p.w[1] = (const uint8_t*)up;
+    p.w_scale[0] = w_scale, p.w_scale[1] = up_scale;
+    p.y = (uint8_t*)y, p.y_scale = y_scale;
+    p.L = tile_list_args(ws, true);
+    p.pitch = g.pitch, p.scale_pitch = fp8_scale_pitch(g.k);
+    p.n = g.n, p.n_pad = g.n_pad, p.y_scale_pitch = fp8_scale_pitch(g.n);
+    p.col_group_big = p.col_group_small = 0;
+    p.hdr = ws.split_hdr + which * kFfnSplitHdr;
+    p.counter = ws.split_counter + which * 2 * kFfnSplitUnits;
+    p.stream = stream;
+    if (up)
+        launch_fp8_shape<256, true>(p, ws, st);
+    else if (g.n_pad % 256 == 0)
+        launch_fp8_shape<256, false>(p, ws, st);
+    else
+        launch_fp8_shape<128, false>(p, ws, st);
+}
+
+static bool fp8_is_thin(int64_t max_rows, int experts) {
+#ifdef CAPMOE_FORCE_THIN
+    return CAPMOE_FORCE_THIN;
+#endif
+    return max_rows <= 16ll * experts;
+}
+
 // The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows.
 static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8Workspace& ws, const void* x,
                                  const int32_t* row_token, const int32_t* expert_offset, const moe_fp8_experts_t& w, void* yp,
@@ -99,6 +133,23 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
     if (!schedule_ready) launch_ffn_schedule(expert_offset, schedule_args(ws.f, up, true, &down, compute_units()), st);
     const bool stream = weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
     const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
+    if (!fp8_is_thin(s.max_rows, d.n_experts)) {
+        {
+            ProfileScope prof(MOE_KERNEL_DISPATCH, st);
+            const hipError_t e = launch_quantize_rows(MOE_DTYPE_BF16, x, x_rows, d.d_model, nullptr,
+                                                      row_token ? nullptr : expert_offset + d.n_experts, ws.xq, ws.xs, st);
+            if (e != hipSuccess) return e;
+        }
+        {
+            ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
+            launch_fp8_tiles(up, ws.f, 0, ws.xq, ws.xs, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden,
+                             ws.hidden_scale, stream, st);
+        }
+        ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
+        launch_fp8_tiles(down, ws.f, 1, ws.f.hidden, ws.hidden_scale, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr,
+                         stream, st);
+        return hipGetLastError();
+    }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
         launch_fp8_thin(up, ws.f, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden, stream, st);
@@ -199,7 +250,11 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
     launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
-    launch_fp8_thin(g, ws.f, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
+    if (!fp8_is_thin(g.max_rows, g.experts))
+        launch_fp8_tiles(g, ws.f, 0, x, x_scale, row_token, w, w_scale, nullptr, nullptr, y, nullptr,
+                         weights_stream((double)g.experts * g.pitch * g.n_pad), st);
+    else
+        launch_fp8_thin(g, ws.f, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
                     weights_stream((double)g.experts * g.pitch * g.n_pad), st);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

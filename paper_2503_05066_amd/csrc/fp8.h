@@ -112,6 +112,25 @@ hipError_t launch_quantize_rows(int dtype, const void* x, int64_t n_rows, int co
 hipError_t launch_quantize_weights(int dtype, const void* w, int experts, int n_out, int n_in, void* q, uint8_t* scale,
                                    hipStream_t st);
 
+// Arguments of the kernels for high row tiles (fp8.hip).
+struct Fp8Args {
+    const uint8_t *x, *x_scale;
+    const int32_t* gather;
+    const uint8_t *w[2], *w_scale[2];  // gate (or the only weights), up
+    uint8_t* y;                        // bf16 rows of n columns; with SWIGLU 8-bit rows of n_pad
+    uint8_t* y_scale;                  // with SWIGLU
+    TileListArgs L;
+    int pitch, scale_pitch;            // of x and of a weight row
+    int n, n_pad, y_scale_pitch;
+    int col_group_big, col_group_small;
+    const int32_t* hdr;
+    int32_t* counter;
+    int stream;
+};
+// One launch over the tiles of a schedule; the shape: 256 weight rows, gate and up rows of 128 columns or not, or 128.
+template <int BN, bool SWIGLU>
+void launch_fp8_shape(Fp8Args p, const FfnWorkspace& ws, hipStream_t st);
+
 // Kernels for tiles of few rows.  x_scale == nullptr: x is bf16 and is quantised as it is read.
 // up != nullptr: the product of the gate and up weights, and y = silu(gate) * up.
 void launch_fp8_thin(const Fp8Gemm& g, const FfnWorkspace& ws, const void* x, const uint8_t* x_scale, int64_t x_rows,
