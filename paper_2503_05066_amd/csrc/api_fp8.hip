@@ -130,10 +130,10 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
                                  bool schedule_ready, hipStream_t st) {
     const int hp = fp8_pitch(d.d_hidden);
     const Fp8Gemm up = fp8_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp8_gemm(d.n_experts, s.max_rows, hp, d.d_model);
-    if (!schedule_ready) launch_ffn_schedule(expert_offset, schedule_args(ws.f, up, true, &down, compute_units()), st);
     const bool stream = weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
     const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
     if (!fp8_is_thin(s.max_rows, d.n_experts)) {
+        if (!schedule_ready) launch_ffn_schedule(expert_offset, schedule_args(ws.f, up, true, &down, compute_units()), st);
         {
             ProfileScope prof(MOE_KERNEL_DISPATCH, st);
             const hipError_t e = launch_quantize_rows(MOE_DTYPE_BF16, x, x_rows, d.d_model, nullptr,
@@ -152,10 +152,10 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
     }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-        launch_fp8_thin(up, ws.f, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden, stream, st);
+        launch_fp8_thin(up, expert_offset, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden, stream, st);
     }
     ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-    launch_fp8_thin(down, ws.f, ws.f.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
+    launch_fp8_thin(down, expert_offset, ws.f.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
     return hipGetLastError();
 }
 
@@ -249,13 +249,14 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
-    launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
-    if (!fp8_is_thin(g.max_rows, g.experts))
-        launch_fp8_tiles(g, ws.f, 0, x, x_scale, row_token, w, w_scale, nullptr, nullptr, y, nullptr,
-                         weights_stream((double)g.experts * g.pitch * g.n_pad), st);
-    else
-        launch_fp8_thin(g, ws.f, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
-                    weights_stream((double)g.experts * g.pitch * g.n_pad), st);
+    const bool streamed = weights_stream((double)g.experts * g.pitch * g.n_pad);
+    if (fp8_is_thin(g.max_rows, g.experts)) {
+        launch_fp8_thin(g, expert_offset, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr,
+                        nullptr, y, streamed, st);
+    } else {
+        launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
+        launch_fp8_tiles(g, ws.f, 0, x, x_scale, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
+    }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -321,7 +322,8 @@ int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_
     const FfnScheduleArgs schedule =
         schedule_args(ws.f, fp8_gemm(desc->n_experts, s.max_rows, desc->d_model, hp), true, &down, compute_units());
     st = capacity_drop_impl(desc, scores, topk_idx, token_class, seed, expert_count, seg_count, expert_offset, row_token,
-                            row_weight, pair_row, workspace, workspace_bytes, s.max_rows > 0 ? &schedule : nullptr, stream);
+                            row_weight, pair_row, workspace, workspace_bytes,
+                            s.max_rows > 0 && !fp8_is_thin(s.max_rows, desc->n_experts) ? &schedule : nullptr, stream);
     if (st != MOE_OK) return st;
     if (s.max_rows > 0) {
         st = ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, true, stream);
