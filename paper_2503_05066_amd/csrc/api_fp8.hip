@@ -95,10 +95,10 @@ static bool weights_stream(double bytes) { return bytes > (double)(320ull << 20)
 
 // One product on the tiles of a schedule (fp8.hip).  which: 0 or 1, its header in the schedule.
 static void launch_fp8_tiles(const Fp8Gemm& g, const FfnWorkspace& ws, int which, const void* x, const uint8_t* x_scale,
-                             const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up,
+                             int64_t x_rows, const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up,
                              const uint8_t* up_scale, void* y, uint8_t* y_scale, bool stream, hipStream_t st) {
     Fp8Args p;
-    p.x = (const uint8_t*)x, p.x_scale = x_scale, p.gather = gather;
+    p.x = (const uint8_t*)x, p.x_scale = x_scale, p.x_rows = x_rows, p.gather = gather;
     p.w[0] = (const uint8_t*)w, p.w[1] = (const uint8_t*)up;
     p.w_scale[0] = w_scale, p.w_scale[1] = up_scale;
     p.y = (uint8_t*)y, p.y_scale = y_scale;
@@ -142,11 +142,11 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
         }
         {
             ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-            launch_fp8_tiles(up, ws.f, 0, ws.xq, ws.xs, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden,
+            launch_fp8_tiles(up, ws.f, 0, ws.xq, ws.xs, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden,
                              ws.hidden_scale, stream, st);
         }
         ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-        launch_fp8_tiles(down, ws.f, 1, ws.f.hidden, ws.hidden_scale, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr,
+        launch_fp8_tiles(down, ws.f, 1, ws.f.hidden, ws.hidden_scale, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr,
                          stream, st);
         return hipGetLastError();
     }
@@ -249,13 +249,14 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
+    const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
     const bool streamed = weights_stream((double)g.experts * g.pitch * g.n_pad);
     if (fp8_is_thin(g.max_rows, g.experts)) {
-        launch_fp8_thin(g, expert_offset, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr,
+        launch_fp8_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr,
                         nullptr, y, streamed, st);
     } else {
         launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
-        launch_fp8_tiles(g, ws.f, 0, x, x_scale, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
+        launch_fp8_tiles(g, ws.f, 0, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

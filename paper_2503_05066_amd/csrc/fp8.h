@@ -115,6 +115,7 @@ hipError_t launch_quantize_weights(int dtype, const void* w, int experts, int n_
 // Arguments of the kernels for high row tiles (fp8.hip).
 struct Fp8Args {
     const uint8_t *x, *x_scale;
+    int64_t x_rows;                    // rows of x
     const int32_t* gather;
     const uint8_t *w[2], *w_scale[2];  // gate (or the only weights), up
     uint8_t* y;                        // bf16 rows of n columns; with SWIGLU 8-bit rows of n_pad

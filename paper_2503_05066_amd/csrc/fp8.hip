@@ -20,32 +20,60 @@ namespace capmoe {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
-template <int F>
+// BYTE: which byte of the scale words
+template <int F, int BYTE>
 __device__ __forceinline__ void acc_mfma8(const i32x8& w, const i32x8& x, uint32_t w_scale, uint32_t x_scale) {
-    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 a[%0:%1], %2, %3, a[%0:%1], %4, %5 op_sel_hi:[0,0,0]" ::"n"(4 * F),
-                 "n"(4 * F + 3), "v"(w), "v"(x), "v"(w_scale), "v"(x_scale));
+    if constexpr (BYTE == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 a[%0:%1], %2, %3, a[%0:%1], %4, %5 op_sel:[0,0,0] op_sel_hi:[0,0,0]" ::"n"(4 * F),
+                     "n"(4 * F + 3), "v"(w), "v"(x), "v"(w_scale), "v"(x_scale));
+    else
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 a[%0:%1], %2, %3, a[%0:%1], %4, %5 op_sel:[1,1,0] op_sel_hi:[0,0,0]" ::"n"(4 * F),
+                     "n"(4 * F + 3), "v"(w), "v"(x), "v"(w_scale), "v"(x_scale));
 }
 
-// The tile of the bf16 kernel with room for an exchange between waves: up to 2 x 32 rows keep one slab less in flight.
+// The tile of the bf16 kernel, and how its slabs lie in LDS: in a ring of units.  A unit holds half of a slab's activation
+// rows and half of its weight rows (tiles with LIVE above 2), or a slab.  Of activation sub-tile pair j (32 rows) and of 32
+// weight rows 4 KB each; half h of the weights is the h-th half of either wave column's sub-tiles (with SWIGLU: gate, up).
 template <int BN_, bool SWIGLU_>
 struct Shape8 : Shape<BN_, SWIGLU_> {
     using Base = Shape<BN_, SWIGLU_>;
-    static __host__ __device__ constexpr int ring(int live) { return live <= 1 ? 4 : (live <= Base::kRingLive ? 3 : 2); }
-    // the last 4 KB of LDS: of low tiles no slot reaches there, of high ones only the third slot of weights, which is
-    // first requested in the loop
-    static constexpr int kExchange = 160 * 1024 - 4096;
-    static_assert(4 * (4096 + Base::B_SLOT) <= kExchange && 3 * (Base::kRingLive * 4096 + Base::B_SLOT) <= kExchange, "exchange");
     static constexpr int kLdsBytes = 160 * 1024;
+    // the last 4 KB: an exchange between waves at the end of an item, while the next item's first units arrive elsewhere
+    static constexpr int kExchange = kLdsBytes - 4096;
+    static constexpr int TH = Base::TN / 2;
+    static_assert(Base::A_LOADS == 8, "a request per sub-tile pair");
+    static constexpr int kHalfLoads = Base::B_LOADS / 2;  // a wave's requests for half of a slab's weights
+    static __host__ __device__ constexpr bool parts(int live) { return live > 2; }
+    static __host__ __device__ constexpr int half0(int live) { return (live + 1) / 2; }  // sub-tile pairs in the first half
+    static __host__ __device__ constexpr int a_bytes(int live) { return (parts(live) ? half0(live) : live) * 4096; }
+    static __host__ __device__ constexpr int unit(int live) { return a_bytes(live) + (parts(live) ? Base::B_SLOT / 2 : Base::B_SLOT); }
+    static __host__ __device__ constexpr int units(int live) {  // in the ring
+        const int n = (parts(live) ? kLdsBytes : kExchange) / unit(live), most = parts(live) ? 6 : 4;
+        return n < most ? n : most;
+    }
+    // of these, how many are requested before the exchange is over
+    static __host__ __device__ constexpr int early(int live) { return units(live) * unit(live) <= kExchange ? units(live) : units(live) - 1; }
+    static_assert(units(8) >= 5 && units(1) >= 3 && units(2) >= 3 && early(8) * unit(8) <= kExchange, "ring");
+    // slabs at the end of an item that run without some of the requests
+    static __host__ __device__ constexpr int tail(int live) { return parts(live) ? 3 : units(live); }
+    // which half of the activations the first slab of an item begins with: such that the tail always begins with the first
+    static __host__ __device__ constexpr int parity(int live, int slabs) {
+        const int left = slabs - tail(live);
+        return (left > 0 ? left : -left) & 1;
+    }
 };
 
 // What a wave needs to request its pieces of a K slab (see Fills in ffn_tile.h) and the scales.
 template <class S>
 struct Fills8 {
     __amdgpu_buffer_rsrc_t a, b0, b1, sa, sb0, sb1;
-    uint32_t va[S::A_LOADS], vb;  // of the weights the rows of load i lie 32 * i rows further
+    typedef __attribute__((ext_vector_type(8))) unsigned int u32x8;  // (of an array the compiler would keep a copy in memory)
+    u32x8 va;                     // per sub-tile pair
+    uint32_t vb;                  // of the weights the rows of load i lie 32 * i rows further
     uint32_t vsa[2];              // scales: of the rows of sub-tiles 0..3 and 4..7, a quarter of the wave each
-    int first, slabs, turn;
+    int slabs, turn;
     uint32_t row_step;            // bytes of 32 weight rows
+    int64_t scale_at;             // of the wave's weights' scales
     uint8_t* smem;
     int wv;
 
@@ -57,17 +85,22 @@ struct Fills8 {
     __device__ __forceinline__ void aim(const WorkItem& w, const Fp8Args& p, int lane, int wm, int wn) {
         const int32_t* gather = p.gather;
         a = __builtin_amdgcn_make_buffer_rsrc((void*)(gather ? p.x : p.x + (size_t)w.row0 * p.pitch), 0, -1, kRsrcFlags);
-        sa = __builtin_amdgcn_make_buffer_rsrc((void*)(gather ? p.x_scale : p.x_scale + (size_t)w.row0 * p.scale_pitch), 0, -1, kRsrcFlags);
+        const int64_t x0 = gather ? 0 : w.row0;
+        sa = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x_scale + x0 * p.scale_pitch), 0,
+                                               (int)(uint32_t)min((p.x_rows - x0) * p.scale_pitch, (int64_t)kBeyond), kRsrcFlags);
         const size_t n_at = (size_t)w.e * p.n_pad + w.n0;
         b0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[0] + n_at * p.pitch), 0, -1, kRsrcFlags);
         b1 = S::SWIGLU ? __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[1] + n_at * p.pitch), 0, -1, kRsrcFlags) : b0;
         // a wave's weight rows lie in one block of 128 (with SWIGLU in one of either tensor)
-        const size_t s_at = (n_at / kFp8Block + (S::SWIGLU || S::BN == 128 ? 0 : wn)) * p.scale_pitch;
-        sb0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w_scale[0] + s_at), 0, -1, kRsrcFlags);
-        sb1 = S::SWIGLU ? __builtin_amdgcn_make_buffer_rsrc((void*)(p.w_scale[1] + s_at), 0, -1, kRsrcFlags) : sb0;
-        first = w.first;
-        slabs = w.slabs;
-        turn = w.turn;
+        scale_at = (n_at / kFp8Block + (S::SWIGLU || S::BN == 128 ? 0 : wn)) * p.scale_pitch;
+        sb0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w_scale[0] + scale_at), 0, p.scale_pitch, kRsrcFlags);
+        sb1 = S::SWIGLU ? __builtin_amdgcn_make_buffer_rsrc((void*)(p.w_scale[1] + scale_at), 0, p.scale_pitch, kRsrcFlags) : sb0;
+        slabs = __builtin_amdgcn_readfirstlane(w.slabs);
+        turn = __builtin_amdgcn_readfirstlane(w.turn);
+        // the pairs of slabs that share a request for scales (see Scales8) neither wrap around, so that slabs - turn + parity is
+        // even, nor begin an item in two words
+        turn = (turn & ~3) + (S::tail((w.rows + 31) >> 5) & min(turn, 1));
+        turn = __builtin_amdgcn_readfirstlane(turn < slabs ? turn : 0);
         uint32_t row[S::A_LOADS], srow[2];
 #pragma unroll
         for (int i = 0; i < S::A_LOADS; ++i) {
@@ -91,61 +124,100 @@ struct Fills8 {
     }
     __device__ __forceinline__ int slab_at(int kt) const {
         kt += turn;
-        return (kt < slabs ? kt : kt - slabs) + first;
+        return kt < slabs ? kt : kt - slabs;
     }
-    __device__ __forceinline__ void one_a(int i, uint32_t k, int slot) const {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lptr_t)(smem + slot + (wv + S::NW * i) * 1024), 16, va[i], k, 0, 0);
+    // sub-tile pair j of the activations at k bytes of their rows, to byte `to` of LDS
+    __device__ __forceinline__ void one_a(int j, uint32_t k, int to) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lptr_t)(smem + to + wv * 1024), 16, va[j], k, 0, 0);
     }
-    __device__ __forceinline__ void one_b(int i, uint32_t k, int slot, bool once) const {
+    // request i of half h of the weights
+    __device__ __forceinline__ void one_b(int h, int i, uint32_t k, int to, bool once) const {
         // i and once are compile-time constants after unrolling
-        uint8_t* dst = smem + slot + (wv + S::NW * i) * 1024;
-        const bool second = S::SWIGLU && i >= S::B_LOADS / 2;
-        const __amdgpu_buffer_rsrc_t r = second ? b1 : b0;
-        const uint32_t at = k + (uint32_t)(second ? i - S::B_LOADS / 2 : i) * row_step;
+        constexpr int kPer = S::TH / 2;  // 32-row steps of one wave column's half
+        uint8_t* dst = smem + to + (wv + S::NW * i) * 1024;
+        const __amdgpu_buffer_rsrc_t r = S::SWIGLU && h ? b1 : b0;
+        const uint32_t at = k + (uint32_t)(S::SWIGLU ? i : i / kPer * (S::BN / 64) + h * kPer + i % kPer) * row_step;
         if (once)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lptr_t)dst, 16, vb, at, 0, 2);  // bit 1: non-temporal
         else
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lptr_t)dst, 16, vb, at, 0, 0);
     }
-    // The first slabs of an item, as many as its loop keeps whole in LDS.  Returns how many requests are younger than those
-    // of the first slab.
+    // The first units of an item, as many as may be requested while the item before is written.  Returns how many requests are
+    // younger than those of the first.
     __device__ __forceinline__ int start(int live, bool once) const {
-        const int n = min(S::ring(live), slabs);
-        for (int kt = 0; kt < n; ++kt) {
-            const int sa_ = kt * S::a_stride(live), sb_ = S::b_base(live) + kt * S::b_stride(live);
-            const uint32_t k = (uint32_t)slab_at(kt) * 128u;
-            if (once) {
+        const bool parts = S::parts(live);
+        const int h0 = S::half0(live), parity = S::parity(live, slabs);
+        const int n = min(S::early(live), parts ? 2 * slabs : slabs);
+        int younger = 0;
+        for (int u = 0; u < n; ++u) {
+            const int s = parts ? u >> 1 : u, late = parts ? u & 1 : 0, h = late ^ ((s + parity) & 1), to = u * S::unit(live);
+            const uint32_t k = (uint32_t)slab_at(s) * 128u;
+            int count = 0;
 #pragma unroll
-                for (int i = 0; i < S::B_LOADS; ++i) one_b(i, k, sb_, true);
-            } else {
+            for (int hb = 0; hb < 2; ++hb) {
+                if (parts && hb != late) continue;
+                const int base = to + S::a_bytes(live) + (parts ? 0 : hb * (S::Base::B_SLOT / 2));
+                if (once) {
 #pragma unroll
-                for (int i = 0; i < S::B_LOADS; ++i) one_b(i, k, sb_, false);
+                    for (int i = 0; i < S::kHalfLoads; ++i) one_b(hb, i, k, base, true);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < S::kHalfLoads; ++i) one_b(hb, i, k, base, false);
+                }
+                count += S::kHalfLoads;
             }
+            const int lo = parts && h ? h0 : 0, hi = parts && !h ? h0 : live;
 #pragma unroll
-            for (int i = 0; i < S::A_LOADS; ++i)
-                if (i < live) one_a(i, k, sa_);
+            for (int j = 0; j < S::A_LOADS; ++j)
+                if (j >= lo && j < hi) one_a(j, k, to + (j - lo) * 4096);
+            count += hi - lo;
+            if (u > 0) younger += count;
             __builtin_amdgcn_sched_barrier(0);  // their order is what the waits count
         }
-        return (n - 1) * (S::B_LOADS + live);
+        return younger;
     }
 };
 
-// The scales of four slabs (a dword of scale bytes) at a time: those in use and the next ones, requested four slabs ahead.
+// The scales of two slabs at a time, one that begins with either half of the activations (see MatrixLoop8).  Their bytes lie in
+// two words.  They are requested while the two slabs before are multiplied, whether those shared the words or not, and become
+// one word at the end of these: no request for a register is in flight around the loop, nor across the start of an item, where
+// the compiler, which cannot know how many requests are younger, would wait for all of them (once every four slabs, before).
+// An item's first words come through LDS, like its first units.
 template <class S>
 struct Scales8 {
-    uint32_t raw[2], raw_w[2];    // next: of 64 rows each, a row per lane; of the weights, the same in all lanes
-    uint32_t w[2];                // in use
-    __device__ __forceinline__ void request(const Fills8<S>& f, int slab, int live) {
-        const uint32_t at = (uint32_t)(slab >> 2) * 4u;
-        raw[0] = __builtin_amdgcn_raw_buffer_load_b32(f.sa, f.vsa[0], at, 0);
-        if (live > 4) raw[1] = __builtin_amdgcn_raw_buffer_load_b32(f.sa, f.vsa[1], at, 0);
-        raw_w[0] = __builtin_amdgcn_raw_buffer_load_b32(f.sb0, 0, at, 0);
-        if (S::SWIGLU) raw_w[1] = __builtin_amdgcn_raw_buffer_load_b32(f.sb1, 0, at, 0);
+    typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+    u32x2 raw[2], raw_w[2];    // of 64 rows each, a row per lane; of the weights, the same in all lanes
+    uint32_t word[2], word_w[2];  // of the next two slabs, in the lowest bytes
+    static constexpr int kFirst = S::kExchange + 2048;  // [wave][64-row part][lane]
+
+    // an item's first words
+    __device__ __forceinline__ void begin(const Fills8<S>& f) {
+        const int at = f.slab_at(0) & ~3;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f.sa, (lptr_t)(f.smem + kFirst + f.wv * 512 + h * 256), 4, f.vsa[h], at, 0, 0);
     }
-    // the slab after the last one that shares its dword with `slab`
-    static __device__ __forceinline__ int following(const Fills8<S>& f, int slab) {
-        const int next = (slab | 3) + 1;
-        return next < f.first + f.slabs ? next : f.first;
+    // .. once they are in LDS
+    __device__ __forceinline__ void take_first(const Fills8<S>& f, const Fp8Args& p, int64_t w_at, int lane) {
+        const int slab = f.slab_at(0), sh = (slab & 3) * 8;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) word[h] = (uint32_t)*lds_word(f.smem, kFirst + f.wv * 512 + h * 256 + lane * 4) >> sh;
+        word_w[0] = (uint32_t)scalar_word((const int32_t*)(p.w_scale[0] + w_at), slab >> 2) >> sh;
+        if (S::SWIGLU) word_w[1] = (uint32_t)scalar_word((const int32_t*)(p.w_scale[1] + w_at), slab >> 2) >> sh;
+    }
+    __device__ __forceinline__ void request(const Fills8<S>& f, int slab) {
+        const uint32_t at = (uint32_t)(slab >> 2) * 4u;
+        raw[0] = __builtin_amdgcn_raw_buffer_load_b64(f.sa, f.vsa[0], at, 0);
+        raw[1] = __builtin_amdgcn_raw_buffer_load_b64(f.sa, f.vsa[1], at, 0);
+        raw_w[0] = __builtin_amdgcn_raw_buffer_load_b64(f.sb0, 0, at, 0);
+        if (S::SWIGLU) raw_w[1] = __builtin_amdgcn_raw_buffer_load_b64(f.sb1, 0, at, 0);
+    }
+    __device__ __forceinline__ void take(int slab) {  // the slab that was asked for
+        const uint32_t sh = (uint32_t)slab & 3u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) word[h] = __builtin_amdgcn_alignbyte(raw[h][1], raw[h][0], sh);
+#pragma unroll
+        for (int u = 0; u < (S::SWIGLU ? 2 : 1); ++u) word_w[u] = __builtin_amdgcn_alignbyte(raw_w[u][1], raw_w[u][0], sh);
     }
 };
 // v holds a value per lane of four groups of 16: out[g] gets group g's in all four groups
@@ -162,28 +234,26 @@ __device__ __forceinline__ void spread(uint32_t v, uint32_t (&out)[4]) {
 // each.  Two sets of both do not fit, so tiles with LIVE above 2 walk a slab in four parts, halves of the activations (A0, A1)
 // by halves of the weights (B0, B1), in turn
 //     A0 B0 | A1 B0 | A1 B1 | A0 B1      then      A1 B0 | A0 B0 | A0 B1 | A1 B1
-// where every half is read anew as soon as its second part is done: B0 of the next slab in the third part, the next slab's
-// first half of A in the fourth, the other half of A in the slab's own first part, B1 in its first two.  So a slab leaves LDS
-// in the middle of its instructions:
-//     parts 1, 2 | barrier kt (slab kt+1 landed, slab kt no longer read) | parts 3, 4 and the requests
-// Tiles with fewer rows hold two sets of operands; they read slab kt+1 while they multiply slab kt, behind a barrier that
-// lies after the first quarter of its instructions.
-// The slots of slab kt are free from barrier kt on: high tiles request the activations of slab kt+2 (two slots) and the weights
-// of slab kt+3 (three), low ones all of slab kt+R (see ring).  Requests complete in order: at barrier kt the weights of slab
-// kt+2 (the slabs kt+2 .. kt+R-1) may still fly.
+// where every half is read anew as soon as its second part is done: the slab's other half of A and B1 in its first two parts,
+// B0 and the first half of A of the next slab in the last two.  Either pair is a unit of the ring (see Shape8), which
+// therefore stays in LDS for half a slab only:
+//     barrier (unit v landed, unit v-1 no longer read) | two parts, operand reads of unit v, requests for unit v-1 + ring
+// With five units of 32 KB a request has four half slabs to land in.  With slabs as units (two slots for the activations,
+// three for the weights, one barrier a slab) it had two to four: 403 us for 7496 rows of 8 x 14336 x 4096, where requests
+// that always hit the L2 took 318.
+// Tiles with fewer rows hold two sets of operands and read slab kt+1 while they multiply slab kt, behind a barrier that lies
+// after the first quarter of its instructions; their units are slabs.
+// Requests complete in order, so the waits count the requests of the units that may still fly.
 template <class S, bool ONCE>
 struct MatrixLoop8 {
     const Fills8<S>& fills;
     Scales8<S>& scales;
-    int a_lane, b_lane;  // byte offset, inside a slot, of this lane's first piece of the wave's first row
+    int a_lane, b_lane;  // byte offset, inside a unit's activations and half of weights, of this lane's first piece
 
-    static __device__ __forceinline__ constexpr int b_tile(int i) {
-        return S::SWIGLU ? ((i / (S::TN / 2)) * (S::BN / 2) + (i % (S::TN / 2)) * 16) * 128 : i * 16 * 128;
-    }
-    // where a slab's operands of this lane lie in LDS: the first and, four pieces further, the second half of a row's 128 bytes
+    // where a unit's operands of this lane lie in LDS: the first and, four pieces further, the second half of a row's 128 bytes
     struct From {
         const uint8_t *lo, *hi;
-        __device__ __forceinline__ From(const uint8_t* slot, int lane_at) : lo(slot + lane_at), hi(slot + (lane_at ^ 64)) {}
+        __device__ __forceinline__ From(const uint8_t* base, int lane_at) : lo(base + lane_at), hi(base + (lane_at ^ 64)) {}
         __device__ __forceinline__ void fetch(i32x8& to, int at) const {
             const u32x4 a = *(const u32x4*)(lo + at), b = *(const u32x4*)(hi + at);
             to = __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -193,213 +263,189 @@ struct MatrixLoop8 {
     // PHASE, draw, before_last: as in ffn.hip
     template <int LIVE, int PHASE, class D, class F>
     __device__ __forceinline__ void run(D&& draw, F&& before_last) {
-        constexpr int TN = S::TN, B_LOADS = S::B_LOADS, NM = TN * LIVE;
-        constexpr int R = S::ring(LIVE);
-        constexpr bool RING = LIVE <= S::kRingLive, PARTS = LIVE > 2;
-        constexpr int SETS = PARTS ? 1 : 2;
-        constexpr int PER = B_LOADS + LIVE;      // requests per slab
-        constexpr int TAIL = RING ? R : 3;       // slabs at the end that run without some of the requests
-        constexpr int A_STRIDE = S::a_stride(LIVE), B_STRIDE = S::b_stride(LIVE), B_BASE = S::b_base(LIVE);
-        constexpr int SA = RING ? R : 2, SB = RING ? R : 3;
-        constexpr int QB = PARTS ? NM / 2 : (NM / 4 > 0 ? NM / 4 : 1);  // instructions ahead of the barrier
-        constexpr int TH = TN / 2, H0 = (LIVE + 1) / 2;
-        // instruction q of a slab with parity SET: its activation and weight sub-tile, and how many rows of instructions (of
-        // consecutive q on one activation sub-tile) come before it
+        constexpr int TN = S::TN, TH = S::TH, NM = TN * LIVE, HALF_LOADS = S::kHalfLoads;
+        constexpr bool PARTS = S::parts(LIVE);
+        constexpr int SETS = PARTS ? 1 : 2, STEPS = PARTS ? 2 : 1;  // units per slab
+        constexpr int NU = S::units(LIVE), UNIT = S::unit(LIVE), A_BYTES = S::a_bytes(LIVE), TAIL = S::tail(LIVE), H0 = S::half0(LIVE);
+        // instruction q of a slab that begins with half `set` of the activations
         struct At {
-            int j, i, row, first;
+            int j, i;
         };
         auto walk = [](int set, int q) constexpr {
-            if (!PARTS) return At{q / TN, q % TN, q / TN, q % TN == 0};
+            if (!PARTS) return At{q / TN, q % TN};
             const int half[2] = {H0, LIVE - H0}, f = set, n_f = half[f], n_g = half[f ^ 1];
-            const int r = q / TH, i = q % TH;  // row of instructions
+            const int r = q / TH, i = q % TH;
             const int part = r < n_f ? 0 : (r < LIVE ? 1 : (r < LIVE + n_g ? 2 : 3));
             const int in = r - (part == 0 ? 0 : (part == 1 ? n_f : (part == 2 ? LIVE : LIVE + n_g)));
             const int h = part == 0 || part == 3 ? f : f ^ 1;
-            return At{(h == 0 ? 0 : H0) + in, (part < 2 ? 0 : TH) + i, r, i == 0};
+            return At{(h == 0 ? 0 : H0) + in, (part < 2 ? 0 : TH) + i};
         };
-        constexpr int ROWS = PARTS ? 2 * LIVE : LIVE;  // rows of instructions
-        // operand reads of a slab, in order, and where: item r of `count` between instructions lo and hi
-        auto spread_at = [](int r, int count, int lo, int hi) constexpr { return lo + r * (hi - lo) / count; };
-        auto before = [spread_at](int q, int count, int lo, int hi) constexpr {  // items that lie ahead of q
-            int n = 0;
-            while (n < count && spread_at(n, count, lo, hi) < q) ++n;
-            return n;
-        };
+        // unit k (0: the one a slab with parity set begins with): its half of the activations, requests
+        auto half_of = [](int set, int k) constexpr { return (k & 1) ^ ((set + k / 2) & 1); };
+        auto loads_a = [half_of](int set, int k) constexpr { return !PARTS ? LIVE : (half_of(set, k) == 0 ? H0 : LIVE - H0); };
+        auto loads = [loads_a](int set, int k) constexpr { return loads_a(set, k) + (PARTS ? HALF_LOADS : 2 * HALF_LOADS); };
         uint8_t* const smem = fills.smem;
         const int KT = fills.slabs;
         int a_lane = this->a_lane, b_lane = this->b_lane;
         asm volatile("" : "+v"(a_lane), "+v"(b_lane));  // the first operand reads stay here, not ahead of all instances
         i32x8 xa[SETS][LIVE], wb[SETS][TN];
-        uint32_t dist[8];  // scale dwords of the sub-tiles' rows
+        uint32_t dist[8], sw[2];  // scale words of the sub-tiles' rows and of the weights
 
-        auto take_scales = [&](int slab) {  // the next four slabs' scales come into use
+        // the scales of slab kt and the one behind it come into use (second: only the latter begins this pair) and those of the
+        // next pair are requested
+        auto use_scales = [&](int kt, bool second) {
+            const int sh = second ? 8 : 0;
             uint32_t d4[4];
-            spread(scales.raw[0], d4);
+            spread(scales.word[0] << sh, d4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) dist[j] = d4[j];
             if (LIVE > 4) {
-                spread(scales.raw[1], d4);
+                spread(scales.word[1] << sh, d4);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dist[4 + j] = d4[j];
             }
-            scales.w[0] = scales.raw_w[0];
-            if (S::SWIGLU) scales.w[1] = scales.raw_w[1];
-            scales.request(fills, Scales8<S>::following(fills, slab), LIVE);
+            sw[0] = scales.word_w[0] << sh;
+            if (S::SWIGLU) sw[1] = scales.word_w[1] << sh;
+            asm volatile("s_nop 1");  // ahead of the matrix instructions that take them (see accumulators.py)
+            __builtin_amdgcn_sched_barrier(0);
+            kt += second ? 1 : 2;
+            scales.request(fills, fills.slab_at(kt < KT ? kt : 0));
+            __builtin_amdgcn_sched_barrier(0);
         };
-        // item r of what is read ahead of a slab's first instruction (PARTS: its first half of A and B0) or, LATE, in its
-        // first parts (the other half of A and B1), in the order of use
-        auto read_item = [&](auto set_c, auto late_c, auto r_c, const From& a, const From& b) {
-            constexpr int set = decltype(set_c)::value, r = decltype(r_c)::value;
-            constexpr bool late = decltype(late_c)::value;
-            constexpr int s = PARTS ? 0 : set;
+        // Operand read r of unit k of a slab with parity set: its weights, then its activations, in the order of use (without
+        // parts: an activation, the weights, the other activations).
+        auto weights_first = [](int k) constexpr { return PARTS ? k % 2 == 0 : false; };
+        auto read_item = [&](auto set_c, auto k_c, auto r_c, const From& a, const From& b) {
+            constexpr int set = decltype(set_c)::value, k = decltype(k_c)::value, r = decltype(r_c)::value;
             if constexpr (!PARTS) {
-                if constexpr (r == 0)
-                    a.fetch(xa[s][0], 0);
-                else if constexpr (r <= TN)
-                    b.fetch(wb[s][r - 1], b_tile(r - 1));
+                constexpr int s = set ^ (k & 1);
+                if constexpr (r == 0 || r > TN)
+                    a.fetch(xa[s][r == 0 ? 0 : r - TN], (r == 0 ? 0 : r - TN) * 4096);
                 else
-                    a.fetch(xa[s][r - TN], (r - TN) * 2 * 16 * 128);
+                    b.fetch(wb[s][r - 1], (r - 1) / TH * (S::Base::B_SLOT / 2) + (r - 1) % TH * 2048);
             } else {
-                constexpr int h = late ? set ^ 1 : set, from = h == 0 ? 0 : H0, n = h == 0 ? H0 : LIVE - H0;
-                if constexpr (late ? r < n : r >= TH) {
-                    constexpr int j = from + (late ? r : r - TH);
-                    a.fetch(xa[0][j], j * 2 * 16 * 128);
-                } else {
-                    constexpr int i = late ? TH + r - n : r;
-                    b.fetch(wb[0][i], b_tile(i));
-                }
+                constexpr int h = half_of(set, k), n = loads_a(set, k), from = h == 0 ? 0 : H0;
+                constexpr int ra = weights_first(k) ? r - TH : r, rb = weights_first(k) ? r : r - n;
+                if constexpr (ra >= 0 && ra < n)
+                    a.fetch(xa[0][from + ra], ra * 4096);
+                else
+                    b.fetch(wb[0][k % 2 * TH + rb], rb * 2048);
             }
         };
-        auto first_items = [](int set) constexpr { return PARTS ? TH + (set == 0 ? H0 : LIVE - H0) : TN + LIVE; };
-        auto late_items = [](int set) constexpr { return PARTS ? TH + (set == 0 ? LIVE - H0 : H0) : 0; };
-        auto slot_a = [&](int slot) { return From(smem + slot * A_STRIDE, a_lane); };
-        auto slot_b = [&](int slot) { return From(smem + B_BASE + slot * B_STRIDE, b_lane); };
-        auto read_first = [&](auto set_c) {
-            const From a = slot_a(0), b = slot_b(0);
-            each<first_items(decltype(set_c)::value)>([&](auto r_c) { read_item(set_c, std::false_type{}, r_c, a, b); });
+        auto items = [loads_a](int set, int k) constexpr { return loads_a(set, k) + (PARTS ? TH : TN); };
+        // where read r of the unit that is read in step `st` lies among the step's instructions (counted from its barrier)
+        constexpr int LEN = NM / STEPS;                                // instructions of a step
+        constexpr int QB = PARTS ? 1 : (NM / 4 > 0 ? NM / 4 : 1);      // of these, ahead of the barrier
+        auto read_at = [loads_a](int set, int st, int r) constexpr {
+            if (!PARTS) return QB + r * (LEN - QB) / (LIVE + TN);
+            if (st == 0) return QB + r * (LEN - QB - 4) / (loads_a(set, 1) + TH);  // activations, then weights
+            // weights over all of it, an activation sub-tile behind its row of the third part
+            return r < TH ? QB + r * (LEN - QB - 4) / TH : (r - TH + 1) * TH;
         };
-        int kt = 0, sa = 0, sb = 0;
+        int kt = 0, slot = 0;  // of the unit that is read
+        auto up = [](int s) { return s == NU - 1 ? 0 : s + 1; };
         // One slab.  T < 0: all requests are made; otherwise TAIL - T slabs are left, this one included.
         auto slab = [&](auto set_c, auto tail_c) {
             constexpr int SET = decltype(set_c)::value, T = decltype(tail_c)::value;
-            constexpr bool MORE = T < TAIL - 1;
-            constexpr bool FILL_A = T < 0 || (!RING && T == 0), FILL_B = T < 0;
-            constexpr int YOUNGER = T < 0 ? (RING ? (R - 2) * PER : B_LOADS)
-                                          : (RING ? (R - 2 - T > 0 ? (R - 2 - T) * PER : 0) : (T == 0 ? B_LOADS : 0));
-            constexpr int NEXT_SET = SET ^ 1, N_FIRST = first_items(NEXT_SET), N_LATE = late_items(SET);
-            constexpr int FIRST_HI = PARTS ? NM - TH : NM;
-            constexpr int FILLS = FILL_B ? PER : (FILL_A ? LIVE : 0);
-            const int at = fills.slab_at(kt);
-            const int sa1 = sa == SA - 1 ? 0 : sa + 1, sb1 = sb == SB - 1 ? 0 : sb + 1;
-            const uint32_t ka = (uint32_t)fills.slab_at(kt + (RING ? R : 2)) * 128u, kb = (uint32_t)fills.slab_at(kt + (RING ? R : 3)) * 128u;
-            const From a0 = slot_a(sa), b0 = slot_b(sb), a1 = slot_a(sa1), b1 = slot_b(sb1);
-            if (kt > 0 && ((at & 3) == 0 || at == fills.first)) take_scales(at);
-            // the slab's scale byte of each dword, by statements that lie two instructions ahead of its use (see accumulators.py)
-            const uint32_t sh = (uint32_t)(at & 3) * 8u;
-            uint32_t sw[2], sx[2];
-            auto shift = [&](uint32_t& to, uint32_t from) {
-                asm volatile("v_lshrrev_b32 %0, %1, %2" : "=v"(to) : "s"(sh), "v"(from));
-            };
-            shift(sx[0], dist[walk(SET, 0).j]);
-            shift(sw[0], scales.w[0]);
-            if (S::SWIGLU) shift(sw[1], scales.w[1]);
-            asm volatile("s_nop 1");
-            __builtin_amdgcn_sched_barrier(0);
-            each<NM>([&](auto q_c) {
-                constexpr int q = decltype(q_c)::value;
-                constexpr At now = walk(SET, q);
-                if constexpr (q == QB) {
-                    // slab kt+1 has landed for this wave (younger requests may still fly), this wave's operand reads of
-                    // slab kt have returned (the LDS counter is part of the wait)
-                    __builtin_amdgcn_s_waitcnt(waitcnt_vm(YOUNGER));
-                    __builtin_amdgcn_s_barrier();
+            constexpr int L = T < 0 ? 1 << 20 : TAIL - T;
+            if constexpr (SET == 0) use_scales(kt, false);
+            each<STEPS>([&](auto st_c) {
+                constexpr int ST = decltype(st_c)::value;
+                constexpr int K = ST + 1;                                     // the unit that is read in this step
+                constexpr bool MORE = ST + 1 < STEPS || L > 1;                // there is one
+                constexpr int KF = ST + NU;                                   // the unit that is requested
+                constexpr bool FILL = KF < STEPS * (L < 1000 ? L : 1000);
+                constexpr int LEFT = STEPS * (L < 1000 ? L : 1000) - 1 - K;   // units behind the one that is read
+                constexpr int FLY = LEFT < NU - 2 ? (LEFT > 0 ? LEFT : 0) : NU - 2;
+                auto younger = [loads]() constexpr {
+                    int n = 0;
+                    for (int k = K + 1; k <= K + FLY; ++k) n += loads(SET, k);
+                    return n;
+                };
+                constexpr int YOUNGER = younger();
+                static_assert(YOUNGER < 64, "vmcnt");
+                const int fill_slot = slot;  // the unit that was read before
+                slot = up(slot);
+                const From a(smem + slot * UNIT, a_lane), b(smem + slot * UNIT + A_BYTES, b_lane);
+                const uint32_t kf = (uint32_t)fills.slab_at(kt + KF / STEPS) * 128u;
+                each<LEN>([&](auto q_c) {
+                    constexpr int n = decltype(q_c)::value, q = ST * LEN + n;
+                    constexpr At now = walk(SET, q);
+                    if constexpr (n == QB) {
+                        // the unit has landed for this wave (younger requests may still fly), this wave's operand reads of the
+                        // one before have returned (the LDS counter is part of the wait)
+                        __builtin_amdgcn_s_waitcnt(waitcnt_vm(YOUNGER));
+                        __builtin_amdgcn_s_barrier();
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if constexpr (MORE && n >= QB) {
+                        constexpr int N = items(SET, K);
+                        each<N>([&](auto r_c) {
+                            if constexpr (read_at(SET, ST, decltype(r_c)::value) == n) read_item(set_c, std::integral_constant<int, K>{}, r_c, a, b);
+                        });
+                    }
+                    if constexpr (FILL && n >= QB) {
+                        constexpr int N = loads(SET, KF), NA = loads_a(SET, KF), H = half_of(SET, KF);
+                        each<N>([&](auto f_c) {
+                            constexpr int f = decltype(f_c)::value;
+                            if constexpr (QB + (4 * f + PHASE) * (LEN - QB) / (4 * N) == n) {
+                                if constexpr (f < NA)
+                                    fills.one_a((PARTS && H ? H0 : 0) + f, kf, fill_slot * UNIT + f * 4096);
+                                else
+                                    fills.one_b(PARTS ? KF % 2 : (f - NA) / HALF_LOADS, (f - NA) % HALF_LOADS, kf,
+                                                fill_slot * UNIT + A_BYTES + (PARTS ? 0 : (f - NA) / HALF_LOADS * (S::Base::B_SLOT / 2)), ONCE);
+                            }
+                        });
+                    }
+                    constexpr int s = PARTS ? 0 : SET;
+                    acc_mfma8<S::fragment(now.i, now.j), SET>(wb[s][now.i], xa[s][now.j], sw[S::SWIGLU ? now.i / TH : 0], dist[now.j]);
                     __builtin_amdgcn_sched_barrier(0);
-                }
-                // reads behind the barrier: of the next slab; ahead of it: the rest of this one
-                if constexpr (q < QB && N_LATE > 0) {
-                    constexpr int lo = before(q, N_LATE, 0, QB - 6), hi = before(q + 1, N_LATE, 0, QB - 6);
-                    each<hi - lo>([&](auto r) {
-                        read_item(set_c, std::true_type{}, std::integral_constant<int, lo + decltype(r)::value>{}, a0, b0);
-                    });
-                }
-                if constexpr (MORE && q >= QB) {
-                    // PARTS: B0 over all of it, an activation sub-tile behind its row of part 3
-                    constexpr int N_B = PARTS ? TH : N_FIRST, N_A = N_FIRST - N_B;
-                    constexpr int lo = before(q, N_B, QB, FIRST_HI), hi = before(q + 1, N_B, QB, FIRST_HI);
-                    each<hi - lo>([&](auto r) {
-                        read_item(std::integral_constant<int, NEXT_SET>{}, std::false_type{},
-                                  std::integral_constant<int, lo + decltype(r)::value>{}, a1, b1);
-                    });
-                    if constexpr (N_A > 0 && q > QB && (q - QB) % TH == 0 && (q - QB) / TH <= N_A)
-                        read_item(std::integral_constant<int, NEXT_SET>{}, std::false_type{},
-                                  std::integral_constant<int, N_B + (q - QB) / TH - 1>{}, a1, b1);
-                }
-                if constexpr (FILLS > 0 && q >= QB) {
-                    auto pos = [](int f) constexpr { return QB + (4 * f + PHASE) * (NM - QB) / (4 * PER); };
-                    auto ahead = [pos](int to) constexpr {
-                        int n = 0;
-                        while (n < FILLS && pos(n) < to) ++n;
-                        return n;
-                    };
-                    constexpr int lo = ahead(q), hi = ahead(q + 1);
-                    each<hi - lo>([&](auto r) {
-                        constexpr int f = lo + decltype(r)::value;
-                        if constexpr (f < LIVE)
-                            fills.one_a(f, ka, sa * A_STRIDE);
-                        else
-                            fills.one_b(f - LIVE, kb, B_BASE + sb * B_STRIDE, ONCE);
-                    });
-                }
-                if constexpr (now.first && now.row + 1 < ROWS) {  // the next row's scales
-                    constexpr int ahead = q + (PARTS ? TH : TN);
-                    shift(sx[(now.row + 1) & 1], dist[walk(SET, ahead).j]);
-                }
-                constexpr int s = PARTS ? 0 : SET;
-                acc_mfma8<S::fragment(now.i, now.j)>(wb[s][now.i], xa[s][now.j], sw[S::SWIGLU ? now.i / TH : 0], sx[now.row & 1]);
-                __builtin_amdgcn_sched_barrier(0);
+                });
             });
-        };
-        auto advance = [&]() {
             ++kt;
-            sa = sa == SA - 1 ? 0 : sa + 1;
-            sb = sb == SB - 1 ? 0 : sb + 1;
+            if constexpr (SET == 1) scales.take(fills.slab_at(kt < KT ? kt : 0));
         };
         using zero = std::integral_constant<int, 0>;
         using one = std::integral_constant<int, 1>;
         using steady = std::integral_constant<int, -1>;
-        take_scales(fills.slab_at(0));
+        auto begin = [&](auto set_c) {
+            constexpr int set = decltype(set_c)::value;
+            if constexpr (set == 1) use_scales(0, true);
+            const From a(smem, a_lane), b(smem + A_BYTES, b_lane);
+            each<items(set, 0)>([&](auto r_c) { read_item(set_c, zero{}, r_c, a, b); });
+            if constexpr (S::early(LIVE) < NU) {  // the ring's last unit, whose place the exchange had
+                constexpr int K = NU - 1, H = half_of(set, K), NA = loads_a(set, K);
+                static_assert(PARTS, "a unit is half a slab");
+                if (K < 2 * KT) {
+                    const uint32_t k = (uint32_t)fills.slab_at(K / 2) * 128u;
+                    each<NA>([&](auto f) { fills.one_a((H ? H0 : 0) + decltype(f)::value, k, K * UNIT + decltype(f)::value * 4096); });
+                    each<HALF_LOADS>([&](auto f) { fills.one_b(K % 2, decltype(f)::value, k, K * UNIT + A_BYTES, ONCE); });
+                }
+            }
+        };
         int left = KT - TAIL;  // slabs with all requests
         const int skip = left < 0 ? -left : 0;
-        if ((left > 0 ? left : skip) & 1)
-            read_first(one{});
+        if (S::parity(LIVE, KT))
+            begin(one{});
         else
-            read_first(zero{});
-        if (!RING && KT > 2) {  // the third slot of weights
-            const uint32_t k = (uint32_t)fills.slab_at(2) * 128u;
-#pragma unroll
-            for (int f = 0; f < B_LOADS; ++f) fills.one_b(f, k, B_BASE + 2 * B_STRIDE, ONCE);
-        }
+            begin(zero{});
         __builtin_amdgcn_sched_barrier(0);
         if (left > 0 && (left & 1)) {
             slab(one{}, steady{});
-            advance();
             --left;
         }
         for (; left > 0; left -= 2) {
             slab(zero{}, steady{});
-            advance();
             slab(one{}, steady{});
-            advance();
         }
         draw();
         each<TAIL>([&](auto t_c) {
             constexpr int t = decltype(t_c)::value;
             if (t < skip) return;
-            // the slot of the slab before is read no more; a product of one slab has the second slot free
-            if (t == TAIL - 1) before_last((kt == 0 ? 1 : (sa == 0 ? SA - 1 : sa - 1)) * A_STRIDE);
+            // the place of a unit that is read no more; a product of one slab leaves the third (with slabs as units the second) free
+            if (t == TAIL - 1) before_last((kt == 0 ? STEPS : (slot == 0 ? NU - 1 : slot - 1)) * UNIT);
             __builtin_amdgcn_sched_barrier(0);
             slab(std::integral_constant<int, t & 1>{}, t_c);
-            advance();
         });
         // the last matrix instructions retire before anything else reads the accumulators
         asm volatile("s_nop 15\n\ts_nop 15");
@@ -529,7 +575,7 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
     const int lr = lane & 15, lk = lane >> 4;
     const int piece0 = (lk ^ ((lr >> 1) & 7)) << 4;
     const int a_lane = (wm * 16 + lr) * 128 + piece0;
-    const int b_lane = ((S::SWIGLU ? wn * (S::BN / 4) : wn * (S::BN / 2)) + lr) * 128 + piece0;
+    const int b_lane = (wn * S::TH * 16 + lr) * 128 + piece0;
 
     Fills8<S> fills;
     Scales8<S> scales;
@@ -537,7 +583,7 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
     fills.wv = wv;
     fills.weights_of_lane(lane, p.pitch);
     fills.aim(cur, p, lane, wm, wn);
-    scales.request(fills, fills.slab_at(0), (cur.rows + 31) >> 5);
+    scales.begin(fills);
     __builtin_amdgcn_sched_barrier(0);
     int younger = fills.start((cur.rows + 31) >> 5, cur.once);
     for (;;) {
@@ -548,6 +594,9 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
         });
         __builtin_amdgcn_sched_barrier(0);
         wait_for_all_but(younger);
+        __builtin_amdgcn_sched_barrier(0);
+        scales.take_first(fills, p, fills.scale_at, lane);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));  // read ahead of the barrier: the ring's last unit may go there
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         // The block's next position.  (The offset of zero is one that the compiler takes for a value per lane: see ffn.hip.)
@@ -602,7 +651,7 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
         younger = 0;
         if (nxt.valid) {
             fills.aim(nxt, p, lane, wm, wn);
-            scales.request(fills, fills.slab_at(0), (nxt.rows + 31) >> 5);
+            scales.begin(fills);
             __builtin_amdgcn_sched_barrier(0);
             younger = fills.start((nxt.rows + 31) >> 5, nxt.once);
         }
