@@ -280,7 +280,7 @@ typedef struct {
     int32_t n_out;      /* columns of y and rows of an expert's weights: a multiple of 8, at most 2^21         */
 } moe_gemm_t;
 
-/* Workspace of moe_grouped_gemm_fp8 (host only). */
+/* Workspace of moe_grouped_gemm_fp8 (host only): 0 bytes, and then `workspace` may be NULL. */
 int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes);
 
 /*

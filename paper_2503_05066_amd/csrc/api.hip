@@ -87,14 +87,21 @@ DropWorkspace drop_workspace(const moe_desc_t& d, const Sizes& s, void* base) {
     return w;
 }
 
-// Tile lists, split headers, tickets and partial tiles of the expert products from byte `off` of the workspace on.
-void place_schedule(FfnWorkspace& w, char* p, size_t& off, int experts, int64_t max_rows, bool mfma_tiles, bool partials) {
-    w.big.tile_m = mfma_tiles ? kFfnTileM : kFfnTileMF32;
-    w.big.max_tiles = (int)(max_rows / w.big.tile_m) + experts;
+FfnWorkspace ffn_workspace(const moe_desc_t& d, const Sizes& s, void* base) {
+    FfnWorkspace w;
+    char* p = (char*)base;
+    size_t off = 0;
+    const bool bf16 = d.dtype == MOE_DTYPE_BF16;
+    w.big.tile_m = bf16 ? kFfnTileM : kFfnTileMF32;
+
+    w.big.max_tiles = (int)(s.max_rows / w.big.tile_m) + d.n_experts;
     w.small.tile_m = kFfnTileSmall;
-    w.small_max = mfma_tiles ? kFfnSmallMax : 0;
+    w.small_max = bf16 ? kFfnSmallMax : 0;
     // remainders: one per expert at most
-    w.small.max_tiles = mfma_tiles ? experts * (kFfnSmallMax / kFfnTileSmall) : 0;
+    w.small.max_tiles = bf16 ? d.n_experts * (kFfnSmallMax / kFfnTileSmall) : 0;
+
+    w.hidden = p + off;
+    off += align256((size_t)(s.max_rows > 0 ? s.max_rows : 1) * d.d_hidden * s.elem);
     // both kinds in one list (the gate/up GEMM's order)
     w.all.tile_m = 0;
     w.all.max_tiles = w.big.max_tiles + w.small.max_tiles;
@@ -112,27 +119,15 @@ void place_schedule(FfnWorkspace& w, char* p, size_t& off, int experts, int64_t 
     w.split_hdr = nullptr;
     w.split_counter = nullptr;
     w.split_partial = nullptr;
-    if (mfma_tiles) {
+    if (bf16) {
         w.split_hdr = (int32_t*)(p + off);
         off += 256;
         w.split_counter = (int32_t*)(p + off);
         off += align256((size_t)4 * kFfnSplitUnits * 4);
-    }
-    if (partials) {
         w.split_partial = (float*)(p + off);
         off += align256((size_t)kFfnSplitUnits * (kFfnTileM + kFfnTileSmall) * 256 * 4);
     }
     w.bytes = off;
-}
-
-FfnWorkspace ffn_workspace(const moe_desc_t& d, const Sizes& s, void* base) {
-    FfnWorkspace w;
-    char* p = (char*)base;
-    size_t off = 0;
-    const bool bf16 = d.dtype == MOE_DTYPE_BF16;
-    w.hidden = p + off;
-    off += align256((size_t)(s.max_rows > 0 ? s.max_rows : 1) * d.d_hidden * s.elem);
-    place_schedule(w, p, off, d.n_experts, s.max_rows, bf16, bf16);
     return w;
 }
 
@@ -161,6 +156,8 @@ static int ffn_shape_supported(const moe_desc_t& d, bool gathered) {
 }  // namespace capmoe
 
 using namespace capmoe;
+
+static bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Scratch memory of moe_route_topk_static: the split-K partial sums of the router GEMM, for callers that can
 // neither allocate nor pass a workspace.  One copy per GPU, held from the moment the library is loaded on it.
@@ -220,10 +217,10 @@ static int route_topk_impl(const moe_desc_t* desc, const void* x, const float* w
 }
 
 // schedule != nullptr: the drop also builds the tile schedule of the expert GEMMs (moe_layer_forward)
-int capmoe::capacity_drop_impl(const moe_desc_t* desc, const float* scores, const int32_t* topk_idx,
-                               const uint8_t* token_class, uint32_t seed, int32_t* expert_count, int32_t* seg_count,
-                               int32_t* expert_offset, int32_t* row_token, float* row_weight, int32_t* pair_row,
-                               void* workspace, size_t workspace_bytes, const FfnScheduleArgs* schedule, void* stream) {
+static int capacity_drop_impl(const moe_desc_t* desc, const float* scores, const int32_t* topk_idx,
+                              const uint8_t* token_class, uint32_t seed, int32_t* expert_count, int32_t* seg_count,
+                              int32_t* expert_offset, int32_t* row_token, float* row_weight, int32_t* pair_row,
+                              void* workspace, size_t workspace_bytes, const FfnScheduleArgs* schedule, void* stream) {
     const int v = validate(desc);
     if (v != MOE_OK) return v;
     if (!expert_count || !seg_count || !expert_offset || !workspace) return MOE_ERR_INVALID_ARG;

@@ -1,71 +1,36 @@
 // The entry points of the 8-bit experts: argument validation, workspace layout, the calls' launches.
 #include <algorithm>
 
-#include "ffn_tile.h"
 #include "fp8.h"
 
 namespace capmoe {
 
-// Workspace of a layer's FFN, or of one product (h == 0: no quantised x, no hidden activation).
+// Workspace of a layer's FFN.  (A product by itself needs none.)
 struct Fp8Workspace {
-    FfnWorkspace f;         // hidden: [P_max, h filled up] bf16, or 8-bit values and behind them their scales
+    void* hidden;           // [P_max, h filled up] bf16, or 8-bit values and behind them their scales
     uint8_t* hidden_scale;
     void* xq;               // [rows of x, pitch]
     uint8_t* xs;
     size_t bytes;
 };
 
-static Fp8Workspace gemm_workspace(const Fp8Gemm& g, void* base) {
-    Fp8Workspace w;
-    size_t off = 0;
-    w.f.hidden = nullptr, w.hidden_scale = nullptr, w.xq = nullptr, w.xs = nullptr;
-    place_schedule(w.f, (char*)base, off, g.experts, g.max_rows, true, false);
-    w.bytes = off;
-    return w;
-}
-
-// `reserve`: bytes at the start that an earlier step of the layer may still use when the schedule is built
-static Fp8Workspace ffn_fp8_workspace(const moe_desc_t& d, const Sizes& s, size_t reserve, void* base) {
+static Fp8Workspace ffn_fp8_workspace(const moe_desc_t& d, const Sizes& s, void* base) {
     Fp8Workspace w;
     char* p = (char*)base;
     size_t off = 0;
     const int64_t rows = std::max<int64_t>(s.max_rows, 1);
-    w.f.hidden = p + off;
-    w.hidden_scale = (uint8_t*)(p + off + align256((size_t)rows * fp8_pitch(d.d_hidden)));
-    off += align256((size_t)rows * fp8_pitch(d.d_hidden)) + align256((size_t)rows * fp8_pitch(d.d_hidden));
+    const size_t hidden = align256((size_t)rows * fp8_pitch(d.d_hidden));
+    w.hidden = p;
+    w.hidden_scale = (uint8_t*)(p + hidden);
+    off += 2 * hidden;
     static_assert(kFp8Block >= 4, "a row's scale bytes fit where its second byte per value would be");
     const int64_t x_rows = std::max<int64_t>(rows, d.n_tokens);
     w.xq = p + off;
     off += align256((size_t)x_rows * fp8_pitch(d.d_model));
     w.xs = (uint8_t*)(p + off);
     off += align256((size_t)x_rows * fp8_scale_pitch(d.d_model));
-    off = std::max(off, align256(reserve));
-    place_schedule(w.f, p, off, d.n_experts, s.max_rows, true, false);
     w.bytes = off;
     return w;
-}
-
-// The tile schedule's arguments for one product or two on the same tiles.
-static FfnScheduleArgs schedule_args(const FfnWorkspace& ws, const Fp8Gemm& first, bool swiglu, const Fp8Gemm* second, int cus) {
-    FfnScheduleArgs a;
-    a.enabled = 1;
-    a.E = first.experts;
-    a.big_sh = 8;
-    a.small_sh = 6;
-    static_assert(kFfnTileM == 1 << 8 && kFfnTileSmall == 1 << 6, "tile heights");
-    a.small_max = ws.small_max;
-    a.cus = cus;
-    a.L = tile_list_args(ws, true);
-    auto columns = [](const Fp8Gemm& g, bool narrow) { return narrow || g.n_pad % 256 != 0 ? g.n_pad / 128 : g.n_pad / 256; };
-    const int c1 = columns(first, swiglu);
-    a.first = SplitArgs{ws.split_hdr, ws.split_counter, c1, c1, std::min(first.pitch / kFp8Block, kFfnSplitMinK - 1)};
-    a.second = a.first;
-    if (second) {
-        const int c2 = columns(*second, false);
-        a.second = SplitArgs{ws.split_hdr + kFfnSplitHdr, ws.split_counter + 2 * kFfnSplitUnits, c2, c2,
-                             std::min(second->pitch / kFp8Block, kFfnSplitMinK - 1)};
-    }
-    return a;
 }
 
 static int validate_gemm(const moe_gemm_t* g) {
@@ -74,6 +39,7 @@ static int validate_gemm(const moe_gemm_t* g) {
     return MOE_OK;
 }
 
+static bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 static bool misaligned4(const void* p) { return ((uintptr_t)p & 3) != 0; }
 
 static int validate_fp8(const moe_desc_t* d) {
@@ -93,8 +59,8 @@ static int validate_experts(const moe_fp8_experts_t* w) {
 
 static bool weights_stream(double bytes) { return bytes > (double)(320ull << 20); }
 
-// One product on the tiles of a schedule (fp8.hip).  which: 0 or 1, its header in the schedule.
-static void launch_fp8_tiles(const Fp8Gemm& g, const FfnWorkspace& ws, int which, const void* x, const uint8_t* x_scale,
+// One product on high row tiles (fp8.hip).
+static void launch_fp8_tiles(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale,
                              int64_t x_rows, const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up,
                              const uint8_t* up_scale, void* y, uint8_t* y_scale, bool stream, hipStream_t st) {
     Fp8Args p;
@@ -102,19 +68,17 @@ static void launch_fp8_tiles(const Fp8Gemm& g, const FfnWorkspace& ws, int which
     p.w[0] = (const uint8_t*)w, p.w[1] = (const uint8_t*)up;
     p.w_scale[0] = w_scale, p.w_scale[1] = up_scale;
     p.y = (uint8_t*)y, p.y_scale = y_scale;
-    p.L = tile_list_args(ws, true);
+    p.expert_offset = expert_offset, p.max_rows = g.max_rows, p.experts = g.experts;
     p.pitch = g.pitch, p.scale_pitch = fp8_scale_pitch(g.k);
     p.n = g.n, p.n_pad = g.n_pad, p.y_scale_pitch = fp8_scale_pitch(g.n);
-    p.col_group_big = p.col_group_small = 0;
-    p.hdr = ws.split_hdr + which * kFfnSplitHdr;
-    p.counter = ws.split_counter + which * 2 * kFfnSplitUnits;
+    p.col_group = 0;
     p.stream = stream;
     if (up)
-        launch_fp8_shape<256, true>(p, ws, st);
+        launch_fp8_shape<256, true>(p, st);
     else if (g.n_pad % 256 == 0)
-        launch_fp8_shape<256, false>(p, ws, st);
+        launch_fp8_shape<256, false>(p, st);
     else
-        launch_fp8_shape<128, false>(p, ws, st);
+        launch_fp8_shape<128, false>(p, st);
 }
 
 static bool fp8_is_thin(int64_t max_rows, int experts) {
@@ -127,13 +91,12 @@ static bool fp8_is_thin(int64_t max_rows, int experts) {
 // The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows.
 static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8Workspace& ws, const void* x,
                                  const int32_t* row_token, const int32_t* expert_offset, const moe_fp8_experts_t& w, void* yp,
-                                 bool schedule_ready, hipStream_t st) {
+                                 hipStream_t st) {
     const int hp = fp8_pitch(d.d_hidden);
     const Fp8Gemm up = fp8_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp8_gemm(d.n_experts, s.max_rows, hp, d.d_model);
     const bool stream = weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
     const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
     if (!fp8_is_thin(s.max_rows, d.n_experts)) {
-        if (!schedule_ready) launch_ffn_schedule(expert_offset, schedule_args(ws.f, up, true, &down, compute_units()), st);
         {
             ProfileScope prof(MOE_KERNEL_DISPATCH, st);
             const hipError_t e = launch_quantize_rows(MOE_DTYPE_BF16, x, x_rows, d.d_model, nullptr,
@@ -142,20 +105,20 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
         }
         {
             ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-            launch_fp8_tiles(up, ws.f, 0, ws.xq, ws.xs, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden,
+            launch_fp8_tiles(up, expert_offset, ws.xq, ws.xs, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden,
                              ws.hidden_scale, stream, st);
         }
         ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-        launch_fp8_tiles(down, ws.f, 1, ws.f.hidden, ws.hidden_scale, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr,
+        launch_fp8_tiles(down, expert_offset, ws.hidden, ws.hidden_scale, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr,
                          stream, st);
         return hipGetLastError();
     }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-        launch_fp8_thin(up, expert_offset, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.f.hidden, stream, st);
+        launch_fp8_thin(up, expert_offset, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, stream, st);
     }
     ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-    launch_fp8_thin(down, expert_offset, ws.f.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
+    launch_fp8_thin(down, expert_offset, ws.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
     return hipGetLastError();
 }
 
@@ -164,9 +127,8 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
 using namespace capmoe;
 
 static int ffn_fp8_impl(const moe_desc_t* desc, const void* x, const int32_t* row_token, const int32_t* expert_offset,
-                        const moe_fp8_experts_t* experts, void* yp, const Fp8Workspace& ws, bool schedule_ready, void* stream) {
-    return launch_ffn_fp8(*desc, derive(*desc), ws, x, row_token, expert_offset, *experts, yp, schedule_ready,
-                          (hipStream_t)stream) == hipSuccess
+                        const moe_fp8_experts_t* experts, void* yp, const Fp8Workspace& ws, void* stream) {
+    return launch_ffn_fp8(*desc, derive(*desc), ws, x, row_token, expert_offset, *experts, yp, (hipStream_t)stream) == hipSuccess
                ? MOE_OK
                : MOE_ERR_HIP;
 }
@@ -181,10 +143,10 @@ static int ffn_fp8_checked(const moe_desc_t* desc, const void* x, const int32_t*
     if (w != MOE_OK) return w;
     if (row_token && (uint64_t)desc->n_tokens * (uint64_t)desc->d_model >= (1ull << 31)) return MOE_ERR_UNSUPPORTED;
     const Sizes s = derive(*desc);
-    const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, 0, workspace);
+    const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, workspace);
     if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (s.max_rows == 0) return MOE_OK;
-    return ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, false, stream);
+    return ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, stream);
 }
 
 extern "C" {
@@ -231,7 +193,7 @@ int moe_quantize_weights(int dtype, const void* w, int32_t n_experts, int32_t n_
 int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes) {
     const int v = validate_gemm(gemm);
     if (v != MOE_OK) return v;
-    if (workspace_bytes) *workspace_bytes = gemm_workspace(fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out), nullptr).bytes;
+    if (workspace_bytes) *workspace_bytes = 0;
     return MOE_OK;
 }
 
@@ -240,13 +202,11 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
                          size_t workspace_bytes, void* stream) {
     const int v = validate_gemm(gemm);
     if (v != MOE_OK) return v;
-    if (!x || !x_scale || !expert_offset || !w || !w_scale || !y || !workspace) return MOE_ERR_INVALID_ARG;
+    if (!x || !x_scale || !expert_offset || !w || !w_scale || !y) return MOE_ERR_INVALID_ARG;
     if (misaligned16(x) || misaligned16(w) || misaligned16(y) || misaligned4(x_scale) || misaligned4(w_scale)) return MOE_ERR_INVALID_ARG;
-    if (((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
+    (void)workspace, (void)workspace_bytes;  // none is needed
     const Fp8Gemm g = fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
-    const Fp8Workspace ws = gemm_workspace(g, workspace);
-    if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
     const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
@@ -255,8 +215,7 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
         launch_fp8_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr,
                         nullptr, y, streamed, st);
     } else {
-        launch_ffn_schedule(expert_offset, schedule_args(ws.f, g, false, nullptr, compute_units()), st);
-        launch_fp8_tiles(g, ws.f, 0, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
+        launch_fp8_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -268,7 +227,7 @@ int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes) {
     const int q = moe_query(desc, nullptr, nullptr, nullptr, &other);
     if (q != MOE_OK) return q;
     const Sizes s = derive(*desc);
-    const size_t mine = ffn_fp8_workspace(*desc, s, drop_workspace(*desc, s, nullptr).bytes, nullptr).bytes;
+    const size_t mine = ffn_fp8_workspace(*desc, s, nullptr).bytes;
     if (workspace_bytes) *workspace_bytes = std::max(mine, other);
     return MOE_OK;
 }
@@ -316,18 +275,11 @@ int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_
     if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
     int st = moe_route_topk(desc, x, w_router, bias, 0, logits, scores, topk_idx, topk_score, workspace, workspace_bytes, stream);
     if (st != MOE_OK) return st;
-    // the last launch of the drop builds the tile schedule of the products, behind what the drop itself uses
-    const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, drop_workspace(*desc, s, nullptr).bytes, workspace);
-    const int hp = fp8_pitch(desc->d_hidden);
-    const Fp8Gemm down = fp8_gemm(desc->n_experts, s.max_rows, hp, desc->d_model);
-    const FfnScheduleArgs schedule =
-        schedule_args(ws.f, fp8_gemm(desc->n_experts, s.max_rows, desc->d_model, hp), true, &down, compute_units());
-    st = capacity_drop_impl(desc, scores, topk_idx, token_class, seed, expert_count, seg_count, expert_offset, row_token,
-                            row_weight, pair_row, workspace, workspace_bytes,
-                            s.max_rows > 0 && !fp8_is_thin(s.max_rows, desc->n_experts) ? &schedule : nullptr, stream);
+    st = moe_capacity_drop_ranked(desc, scores, topk_idx, token_class, seed, expert_count, seg_count, expert_offset, row_token,
+                                  row_weight, pair_row, workspace, workspace_bytes, stream);
     if (st != MOE_OK) return st;
     if (s.max_rows > 0) {
-        st = ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ws, true, stream);
+        st = ffn_fp8_impl(desc, x, row_token, expert_offset, experts, yp, ffn_fp8_workspace(*desc, s, workspace), stream);
         if (st != MOE_OK) return st;
     }
     return moe_combine(desc, yp, row_weight, pair_row, y, stream);

@@ -100,7 +100,6 @@ struct FfnWorkspace {
     size_t bytes;
 };
 FfnWorkspace ffn_workspace(const moe_desc_t& d, const Sizes& s, void* base);
-void place_schedule(FfnWorkspace& w, char* p, size_t& off, int experts, int64_t max_rows, bool mfma_tiles, bool partials);
 
 // The caller's profile table (moe_profile_attach), per host thread; ProfileScope records the table's events
 // around one launch and counts the launch.  The library keeps only this pointer, never the table.
@@ -141,14 +140,6 @@ int compute_units();  // of the current device
 
 struct FfnScheduleArgs;  // schedule.h
 
-// The steps around the expert products, as the entry points and those of the layers with 8-bit experts enqueue them (api.hip).
-// schedule != nullptr: the drop also builds the tile schedule of the expert products.
-int capacity_drop_impl(const moe_desc_t* desc, const float* scores, const int32_t* topk_idx, const uint8_t* token_class,
-                       uint32_t seed, int32_t* expert_count, int32_t* seg_count, int32_t* expert_offset, int32_t* row_token,
-                       float* row_weight, int32_t* pair_row, void* workspace, size_t workspace_bytes,
-                       const FfnScheduleArgs* schedule, void* stream);
-inline bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
-
 // Launchers (each returns a hipError_t from hipGetLastError after its launches).
 hipError_t launch_router_logits(const moe_desc_t& d, const void* x, const float* w, const float* bias, float* logits,
                                 hipStream_t st);
@@ -181,7 +172,6 @@ void launch_ffn_down_f32(const moe_desc_t& d, const Sizes& s, const FfnWorkspace
                          hipStream_t st);
 // schedule != nullptr (launch_capacity_drop): the drop also builds the tile schedule of the expert GEMMs;
 // schedule_ready (launch_grouped_ffn): it has been built that way, no schedule kernel is launched
-void launch_ffn_schedule(const int32_t* expert_offset, const FfnScheduleArgs& args, hipStream_t st);
 FfnScheduleArgs ffn_schedule_args(const moe_desc_t& d, const FfnWorkspace& ws, int cus);
 void ffn_schedule_on_host(const moe_desc_t& d, const FfnWorkspace& ws, const int32_t* expert_count, int cus,
                           int32_t* tiles, int32_t* header);

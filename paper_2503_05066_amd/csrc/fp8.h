@@ -2,7 +2,6 @@
 #pragma once
 
 #include "common.h"
-#include "schedule.h"
 
 namespace capmoe {
 
@@ -120,17 +119,17 @@ struct Fp8Args {
     const uint8_t *w[2], *w_scale[2];  // gate (or the only weights), up
     uint8_t* y;                        // bf16 rows of n columns; with SWIGLU 8-bit rows of n_pad
     uint8_t* y_scale;                  // with SWIGLU
-    TileListArgs L;
+    const int32_t* expert_offset;
+    int64_t max_rows;
+    int experts;
     int pitch, scale_pitch;            // of x and of a weight row
     int n, n_pad, y_scale_pitch;
-    int col_group_big, col_group_small;
-    const int32_t* hdr;
-    int32_t* counter;
-    int stream;
+    int col_group;
+    int stream;                        // the weights' lines need not be kept
 };
-// One launch over the tiles of a schedule; the shape: 256 weight rows, gate and up rows of 128 columns or not, or 128.
+// One launch over all tiles; the shape: 256 weight rows, gate and up rows of 128 columns or not, or 128.
 template <int BN, bool SWIGLU>
-void launch_fp8_shape(Fp8Args p, const FfnWorkspace& ws, hipStream_t st);
+void launch_fp8_shape(Fp8Args p, hipStream_t st);
 
 // Kernels for tiles of few rows.  x_scale == nullptr: x is bf16 and is quantised as it is read.
 // up != nullptr: the product of the gate and up weights, and y = silu(gate) * up.

@@ -228,6 +228,21 @@ __device__ __forceinline__ void spread(uint32_t v, uint32_t (&out)[4]) {
     out[0] = lo[0], out[1] = lo[1], out[2] = hi[0], out[3] = hi[1];
 }
 
+// f(r) for the r in [FROM, N) with at(r) == POS, all known at compile time (at keeps no values)
+template <int FROM, int N, int POS, class At, class F>
+__device__ __forceinline__ void each_at(At at, F&& f) {
+    auto find = [](At where) constexpr {
+        int r = FROM;
+        while (r < N && where(r) != POS) ++r;
+        return r;
+    };
+    constexpr int r = find(at);
+    if constexpr (r < N) {
+        f(std::integral_constant<int, r>{});
+        each_at<r + 1, N, POS>(at, f);
+    }
+}
+
 // K loop of a wave.  LIVE = number of 16-row activation sub-tiles per wave that are fetched and multiplied.
 //
 // A slab is one matrix instruction per pair of sub-tiles, and its operands (a wave's 128 rows of either side) take 64 registers
@@ -260,9 +275,9 @@ struct MatrixLoop8 {
         }
     };
 
-    // PHASE, draw, before_last: as in ffn.hip
-    template <int LIVE, int PHASE, class D, class F>
-    __device__ __forceinline__ void run(D&& draw, F&& before_last) {
+    // PHASE (0..3): where in a step this wave places its requests: the waves leave every barrier together (see ffn.hip)
+    template <int LIVE, int PHASE>
+    __device__ __forceinline__ void run() {
         constexpr int TN = S::TN, TH = S::TH, NM = TN * LIVE, HALF_LOADS = S::kHalfLoads;
         constexpr bool PARTS = S::parts(LIVE);
         constexpr int SETS = PARTS ? 1 : 2, STEPS = PARTS ? 2 : 1;  // units per slab
@@ -379,22 +394,18 @@ struct MatrixLoop8 {
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     if constexpr (MORE && n >= QB) {
-                        constexpr int N = items(SET, K);
-                        each<N>([&](auto r_c) {
-                            if constexpr (read_at(SET, ST, decltype(r_c)::value) == n) read_item(set_c, std::integral_constant<int, K>{}, r_c, a, b);
-                        });
+                        each_at<0, items(SET, K), n>([read_at](int r) constexpr { return read_at(SET, ST, r); },
+                                                     [&](auto r_c) { read_item(set_c, std::integral_constant<int, K>{}, r_c, a, b); });
                     }
                     if constexpr (FILL && n >= QB) {
                         constexpr int N = loads(SET, KF), NA = loads_a(SET, KF), H = half_of(SET, KF);
-                        each<N>([&](auto f_c) {
+                        each_at<0, N, n>([](int f) constexpr { return QB + (4 * f + PHASE) * (LEN - QB) / (4 * N); }, [&](auto f_c) {
                             constexpr int f = decltype(f_c)::value;
-                            if constexpr (QB + (4 * f + PHASE) * (LEN - QB) / (4 * N) == n) {
-                                if constexpr (f < NA)
-                                    fills.one_a((PARTS && H ? H0 : 0) + f, kf, fill_slot * UNIT + f * 4096);
-                                else
-                                    fills.one_b(PARTS ? KF % 2 : (f - NA) / HALF_LOADS, (f - NA) % HALF_LOADS, kf,
-                                                fill_slot * UNIT + A_BYTES + (PARTS ? 0 : (f - NA) / HALF_LOADS * (S::Base::B_SLOT / 2)), ONCE);
-                            }
+                            if constexpr (f < NA)
+                                fills.one_a((PARTS && H ? H0 : 0) + f, kf, fill_slot * UNIT + f * 4096);
+                            else
+                                fills.one_b(PARTS ? KF % 2 : (f - NA) / HALF_LOADS, (f - NA) % HALF_LOADS, kf,
+                                            fill_slot * UNIT + A_BYTES + (PARTS ? 0 : (f - NA) / HALF_LOADS * (S::Base::B_SLOT / 2)), ONCE);
                         });
                     }
                     constexpr int s = PARTS ? 0 : SET;
@@ -438,13 +449,9 @@ struct MatrixLoop8 {
             slab(zero{}, steady{});
             slab(one{}, steady{});
         }
-        draw();
         each<TAIL>([&](auto t_c) {
             constexpr int t = decltype(t_c)::value;
             if (t < skip) return;
-            // the place of a unit that is read no more; a product of one slab leaves the third (with slabs as units the second) free
-            if (t == TAIL - 1) before_last((kt == 0 ? STEPS : (slot == 0 ? NU - 1 : slot - 1)) * UNIT);
-            __builtin_amdgcn_sched_barrier(0);
             slab(std::integral_constant<int, t & 1>{}, t_c);
         });
         // the last matrix instructions retire before anything else reads the accumulators
@@ -467,6 +474,7 @@ struct ColumnWriter {
         const int in = wn * (S::kNCols / 2) + (lk & 1) * 16 + (lk >> 1) * 8;
         col = w.n0 + in;
         at = (uint32_t)(wm * 16 + lr) * pitch + (uint32_t)in * 2u;
+        asm volatile("" : "+v"(at));  // what follows from it is computed for each item, not kept in registers through the loop
     }
     template <class Frag>
     __device__ __forceinline__ void rows(int j, Frag&& frag) const {
@@ -492,6 +500,7 @@ struct ColumnWriter {
 template <class S>
 __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w, int wm, int wn, int lane, int live, uint8_t* smem) {
     constexpr int TM = S::TM;
+    asm volatile("" : "+v"(lane));  // (see ColumnWriter)
     const int lr = lane & 15, lk = lane >> 4;
     uint32_t v[TM][8], bad[TM], top[TM];
     each<TM>([&](auto j_c) {
@@ -542,6 +551,120 @@ __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w,
     return 2 * live;
 }
 
+// The order of the work, found by every wave for itself from the experts' offsets: no launch ahead of this one builds a
+// schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
+//
+// First the full row tiles (256 rows), expert by expert, then what is left of the experts' rows, higher tiles first, so that the
+// last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the XCDs in turn (block id mod 8), and the
+// blocks of an XCD take the items of its chunks in turn.  About as many tiles as an expert has make a chunk: those that run
+// together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
+// (A ticket per item instead of turns: the same within 2 % where all items are alike, and counters that somebody has to clear.)
+template <class S>
+struct TileOrder {
+    static constexpr int kChunks = kMaxExperts / kWave;
+    const int32_t* offset;
+    int ends[kChunks];  // of expert 64 c + lane: full tiles up to and including its own
+    uint32_t parts;     // of place 64 c + lane among the partly filled tiles: its expert, in byte c
+    int full, tiles, slabs, n_pad, group, deal, row_chunks, chunks;
+    bool stream;
+
+    __device__ __forceinline__ TileOrder(const Fp8Args& p, int lane, uint8_t* scratch)
+        : offset(p.expert_offset), slabs(p.pitch / kFp8Block), n_pad(p.n_pad), group(p.col_group), stream(p.stream) {
+        int rows[kChunks];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const int e = c * kWave + lane;
+            const int lo = e < p.experts ? offset[e] : 0, hi = e < p.experts ? offset[e + 1] : 0;
+            rows[c] = hi - lo;
+        }
+        full = 0;
+        int active = 0;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            int n = rows[c] >> 8;
+#pragma unroll
+            for (int off = 1; off < kWave; off <<= 1) {
+                const int o = __shfl_up(n, off, kWave);
+                n += lane >= off ? o : 0;
+            }
+            ends[c] = full + n;
+            full = __builtin_amdgcn_readlane(ends[c], kWave - 1);
+            active += __popcll(__ballot(rows[c] > 0));
+        }
+        // places of the partly filled tiles: by height in steps of 32 rows, then by expert
+        int n_parts = 0;
+        const uint64_t below = ((uint64_t)1 << lane) - 1;
+        auto word = [&](int i) { return (lds_int_t)(scratch + i * 4); };
+#pragma unroll
+        for (int height = 8; height > 0; --height)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const bool mine = ((rows[c] & 255) + 31) >> 5 == height;
+                const uint64_t all = __ballot(mine);
+                if (mine) *word(n_parts + __popcll(all & below)) = c * kWave + lane;
+                n_parts += __popcll(all);
+            }
+        parts = 0;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) parts |= ((uint32_t)*word(c * kWave + lane) & 255u) << (8 * c);
+        tiles = full + n_parts;
+        const int columns = n_pad / S::kNCols;
+        const int each = tiles / max(active, 1);  // tiles of an expert, on average
+        deal = each >= 6 ? 8 : (each >= 3 ? 4 : (each >= 2 ? 2 : 1));
+        row_chunks = (tiles + deal - 1) / deal;
+        chunks = row_chunks * (columns / group);
+    }
+    // position p of this XCD's share; past its end: not valid, `more` false; a place that the last chunk of a column group
+    // leaves empty: not valid, `more` true
+    __device__ __forceinline__ WorkItem at(int xcd, int p, bool& more) const {
+        WorkItem w;
+        w.valid = 0;
+        const int per_chunk = deal * group, j = p / per_chunk, in = p - j * per_chunk;
+        const int chunk = xcd + 8 * j;
+        more = chunk < chunks;
+        if (!more) return w;
+        const int cg = chunk / row_chunks, tr = in / group;
+        int tile = (chunk - cg * row_chunks) * deal + tr, col = cg * group + in - tr * group;
+        tile = __builtin_amdgcn_readfirstlane(tile), col = __builtin_amdgcn_readfirstlane(col);
+        if (tile >= tiles) return w;
+        const bool whole = tile < full;
+        int e = 0, before = 0;
+        if (whole) {
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {  // experts whose full tiles all come before this one
+                const int n = __popcll(__ballot(ends[c] <= tile));
+                e += n;
+                if (n > 0) before = __builtin_amdgcn_readlane(ends[c], n - 1);
+            }
+        } else {
+            const int at = tile - full;
+            e = __builtin_amdgcn_readlane((int)parts, at & (kWave - 1)) >> (8 * (at >> 6)) & 255;
+        }
+        const int lo = scalar_word(offset, e), hi = scalar_word(offset, e + 1);
+        w.valid = 1;
+        w.e = e;
+        w.n0 = col * S::kNCols;
+        w.row0 = whole ? lo + (tile - before) * S::BM : lo + ((hi - lo) & ~(S::BM - 1));
+        w.rows = whole ? S::BM : (hi - lo) & (S::BM - 1);
+        // an expert's only tile, in a layer whose weights the memory-side cache does not keep (see ffn.hip)
+        w.once = stream && hi - lo <= S::BM;
+        w.first = 0;
+        w.slabs = slabs;
+        w.turn = w.once ? (int)((long long)w.n0 * slabs / n_pad) : 0;
+        return w;
+    }
+    // the item at place p or the next one of the same block behind it
+    __device__ __forceinline__ WorkItem next(int xcd, int& p, int step) const {
+        bool more = true;
+        WorkItem w;
+        do {
+            w = at(xcd, p, more);
+            p += step;
+        } while (more && !w.valid);
+        return w;
+    }
+};
+
 // One block per compute unit for the whole launch (see ffn.hip).
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) {
@@ -553,25 +676,12 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
     static_assert(S::TN * S::TM == 64 || S::TN * S::TM == 32, "accumulators");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wv >> 1, wn = wv & 1;
-    int per_xcd = gridDim.x >> 3;
-    asm volatile("" : "+s"(per_xcd));  // kept, not fetched again with every ticket
-    const WorkOrder<S> order(p.L, p.hdr, p.pitch / 2, p.n_pad, p.col_group_big, p.col_group_small, p.stream);
+    const int per_xcd = gridDim.x >> 3, xcd = blockIdx.x & 7;
+    const TileOrder<S> order(p, lane, smem + wv * (kMaxExperts * 4));
     int place = blockIdx.x >> 3;
-    if (order.pool > 0 && place >= order.positions()) {  // nothing left of the XCD's share: it starts in the shared end
-        if (wv == 0) {
-            int n = 0;
-            if (lane == 0)
-                n = WorkOrder<S>::kPoolItem +
-                    __hip_atomic_fetch_add(p.counter + kPoolTicket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            n = __builtin_amdgcn_readfirstlane(n);
-            if (lane < S::NW) *lds_word(smem, lane * 1024) = n;  // a copy per wave, in the quarter that only it overwrites
-        }
-        __syncthreads();
-        place = __builtin_amdgcn_readfirstlane(*lds_word(smem, wv * 1024));
-    }
-    WorkItem cur = order.at(place);
+    WorkItem cur = order.next(xcd, place, per_xcd);
     if (!cur.valid) return;
-    const bool more = order.pool > 0 || order.positions() > per_xcd;  // whether a block may find another item
+    __syncthreads();  // the waves' scratch
     const int lr = lane & 15, lk = lane >> 4;
     const int piece0 = (lk ^ ((lr >> 1) & 7)) << 4;
     const int a_lane = (wm * 16 + lr) * 128 + piece0;
@@ -599,55 +709,31 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));  // read ahead of the barrier: the ring's last unit may go there
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        // The block's next position.  (The offset of zero is one that the compiler takes for a value per lane: see ffn.hip.)
-        int next = __builtin_nondeterministic_value(0), none = 0, handed = 0;
-        asm volatile("" : "+v"(none));
-        auto draw = [&]() {
-            if (more && tid == 0)
-                next = __hip_atomic_fetch_add(p.counter + (blockIdx.x & 7) * (kFfnSplitUnits / 8) + kXcdTicket + none, 1,
-                                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        };
-        auto hand_over = [&](int at) {
-            handed = at + wv * 1024;
-            if (more && wv == 0) {
-                int n = 0;
-                if (lane == 0) {
-                    n = next + per_xcd;
-                    if (order.pool > 0 && n >= order.positions())
-                        n = WorkOrder<S>::kPoolItem +
-                            __hip_atomic_fetch_add(p.counter + kPoolTicket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-                n = __builtin_amdgcn_readfirstlane(n);
-                if (lane < S::NW) *lds_word(smem, at + lane * 1024) = n;
-            }
-        };
         auto loop = [&](auto once_c) {
             MatrixLoop8<S, decltype(once_c)::value> m{fills, scales, a_lane, b_lane};
             switch (live) {
                 case 8:
                     switch (wv) {
-                        case 0: m.template run<8, 0>(draw, hand_over); break;
-                        case 1: m.template run<8, 1>(draw, hand_over); break;
-                        case 2: m.template run<8, 2>(draw, hand_over); break;
-                        default: m.template run<8, 3>(draw, hand_over); break;
+                        case 0: m.template run<8, 0>(); break;
+                        case 1: m.template run<8, 1>(); break;
+                        case 2: m.template run<8, 2>(); break;
+                        default: m.template run<8, 3>(); break;
                     }
                     break;
-                case 7: m.template run<7, 0>(draw, hand_over); break;
-                case 6: m.template run<6, 0>(draw, hand_over); break;
-                case 5: m.template run<5, 0>(draw, hand_over); break;
-                case 4: m.template run<4, 0>(draw, hand_over); break;
-                case 3: m.template run<3, 0>(draw, hand_over); break;
-                case 2: m.template run<2, 0>(draw, hand_over); break;
-                default: m.template run<1, 0>(draw, hand_over); break;
+                case 7: m.template run<7, 0>(); break;
+                case 6: m.template run<6, 0>(); break;
+                case 5: m.template run<5, 0>(); break;
+                case 4: m.template run<4, 0>(); break;
+                case 3: m.template run<3, 0>(); break;
+                case 2: m.template run<2, 0>(); break;
+                default: m.template run<1, 0>(); break;
             }
         };
         if (cur.once)
             loop(std::true_type{});
         else
             loop(std::false_type{});
-        WorkItem nxt;
-        nxt.valid = 0;
-        if (more) nxt = order.at(__builtin_amdgcn_readfirstlane(*lds_word(smem, handed)));
+        const WorkItem nxt = order.next(xcd, place, per_xcd);
         younger = 0;
         if (nxt.valid) {
             fills.aim(nxt, p, lane, wm, wn);
@@ -671,7 +757,7 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
 }
 
 template <int BN, bool SWIGLU>
-void launch_fp8_shape(Fp8Args p, const FfnWorkspace& ws, hipStream_t st) {
+void launch_fp8_shape(Fp8Args p, hipStream_t st) {
     using S = Shape8<BN, SWIGLU>;
     auto kern = fp8_gemm_kernel<S>;
     static std::atomic<uint64_t> configured{0};
@@ -679,23 +765,21 @@ void launch_fp8_shape(Fp8Args p, const FfnWorkspace& ws, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
     });
     const int nb = p.n_pad / S::kNCols;
-    // a block per compute unit, the same number on every XCD; fewer where the plan cannot hold as many items (one that runs
-    // as row pieces is four)
+    // a block per compute unit, the same number on every XCD; fewer where the plan cannot hold as many items
     const int per_xcd = std::max(1, compute_units() / 8);
-    const long long items = (long long)kFfnRowPieces * nb * ((long long)ws.big.max_tiles + ws.small.max_tiles);
+    const long long items = nb * ((long long)(p.max_rows / kFfnTileM) + std::min<long long>(p.max_rows, p.experts));
     const int grid = 8 * (int)std::min<long long>(per_xcd, (items + 7) / 8);
-    p.col_group_big = column_group(nb);
-    p.col_group_small = p.stream ? nb : column_group(nb);
+    p.col_group = nb % 4 == 0 ? 4 : (nb % 3 == 0 ? 3 : (nb % 2 == 0 ? 2 : 1));
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(S::kThreads), S::kLdsBytes, st, p);
 }
 
 // The build compiles this file once for each shape (each takes as long as all other files together).
 #if CAPMOE_FP8_SHAPE == 0
-template void launch_fp8_shape<256, true>(Fp8Args, const FfnWorkspace&, hipStream_t);
+template void launch_fp8_shape<256, true>(Fp8Args, hipStream_t);
 #elif CAPMOE_FP8_SHAPE == 1
-template void launch_fp8_shape<256, false>(Fp8Args, const FfnWorkspace&, hipStream_t);
+template void launch_fp8_shape<256, false>(Fp8Args, hipStream_t);
 #else
-template void launch_fp8_shape<128, false>(Fp8Args, const FfnWorkspace&, hipStream_t);
+template void launch_fp8_shape<128, false>(Fp8Args, hipStream_t);
 #endif
 
 }  // namespace capmoe

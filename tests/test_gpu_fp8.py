@@ -166,6 +166,41 @@ def test_product_through_a_plan(counts, k, n):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("e,k,n", [(256, 256, 264), (130, 136, 512), (65, 384, 1024)])
+def test_product_of_many_experts(e, k, n):
+    g = rng(e)
+    p = Product(list(g.choice([0, 0, 1, 17, 33, 40, 64, 65, 100, 255, 256, 257, 300, 512, 700], e)), k, n)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("counts", [[300, 256, 1, 0, 65, 40, 129, 16, 520, 200, 33, 225], [1, 2, 16, 0, 5, 9, 3, 16, 4, 8, 0, 12]])
+def test_product_whose_weights_are_streamed(counts):
+    # more weights than the memory-side cache holds: other fetch policies, walks over k that begin at different places
+    e, k, n = len(counts), 14336, 2176
+    g = torch.Generator(device="cuda").manual_seed(sum(counts))
+
+    def values(*shape):
+        q = torch.randint(0, 256, shape, generator=g, device="cuda", dtype=torch.uint8)
+        return torch.where((q & 127) > 0x47, q & 0xBF, q)  # magnitudes below 4
+
+    x, w = values(sum(counts), k), values(e, n, k)
+    xs = torch.randint(122, 132, (sum(counts), 112), generator=g, device="cuda", dtype=torch.uint8)
+    ws = torch.randint(122, 132, (e, n // 128, 112), generator=g, device="cuda", dtype=torch.uint8)
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    y = torch.full((sum(counts), n), 7.0, dtype=BF16, device="cuda")
+    gemm = capmoe.make_gemm(sum(counts), k, n, e)
+    capmoe.moe_grouped_gemm_fp8(gemm, x, xs, None, on(offset), w, ws, y, torch.empty(0, dtype=torch.uint8, device="cuda"))
+    f8 = torch.float8_e4m3fn
+    xv = x.view(f8).double() * torch.exp2(xs.double() - 127).repeat_interleave(128, 1)
+    for i in range(e):
+        if counts[i]:
+            wv = w[i].view(f8).double() * torch.exp2(ws[i].double() - 127).repeat_interleave(128, 0).repeat_interleave(128, 1)
+            a = xv[offset[i]:offset[i + 1]]
+            want, mag = a @ wv.T, a.abs() @ wv.abs().T
+            off = (y[offset[i]:offset[i + 1]].double() - want).abs()
+            assert bool((off <= 2.0 ** -8 * want.abs() + 2.0 ** -12 * mag).all()), i
+
+
 @pytest.mark.parametrize("counts,k,n", [([700, 20], 640, 256), ([9, 30], 1024, 136)])
 def test_product_of_values_of_many_sizes(counts, k, n):
     p = Product(counts, k, n, scale_spread=2.0)
