@@ -7,6 +7,7 @@ library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -138,7 +139,7 @@ def make_desc(n_tokens, d_model, n_experts, top_k, d_hidden, device_groups=1, mo
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()  # every argtype is declared, a number will do
 
 
 def _stream(stream):
@@ -146,7 +147,7 @@ def _stream(stream):
         import torch
 
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    return stream.cuda_stream
 
 
 def _check(status: int, what: str):
@@ -241,27 +242,39 @@ def _fits(ok, what):
         raise ValueError(what)
 
 
+_value_dtypes = {}
+
+
 def _value_dtype(t, dims, what):
-    dtype = {"torch.float32": DTYPE_F32, "torch.bfloat16": DTYPE_BF16}.get(str(t.dtype))
-    _fits(dtype is not None and t.dim() == dims and t.is_contiguous(), f"{what}: a dense bf16 or fp32 tensor of {dims} dimensions")
+    if not _value_dtypes:
+        import torch
+
+        _value_dtypes.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, "int32": torch.int32})
+    dtype = _value_dtypes.get(t.dtype)
+    if dtype is None or t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"{what}: a dense bf16 or fp32 tensor of {dims} dimensions")
     return dtype
 
 
 def _fits_fp8(t, shape, what):
-    _fits(tuple(t.shape) == shape and t.element_size() == 1 and t.is_contiguous(), f"{what}: a dense tensor of {shape} bytes")
+    if t.shape != shape or t.element_size() != 1 or not t.is_contiguous():
+        raise ValueError(f"{what}: a dense tensor of {shape} bytes")
+
+
+_fp8_pitches = functools.lru_cache(maxsize=256)(lambda cols: moe_fp8_query(cols))
 
 
 def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
     """x [*, cols] (bf16 or fp32) into the 8-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
     dtype = _value_dtype(x, 2, "x")
     n_rows, cols = q.shape[0], x.shape[1]
-    pitch, scale_pitch = moe_fp8_query(cols)
+    pitch, scale_pitch = _fp8_pitches(cols)
     _fits_fp8(q, (n_rows, pitch), "q")
     _fits_fp8(scale, (n_rows, scale_pitch), "scale")
     if row_token is None:
         _fits(x.shape[0] >= n_rows, "x: a row for every row of q")
     else:
-        _fits(str(row_token.dtype) == "torch.int32" and row_token.numel() >= n_rows and row_token.is_contiguous(),
+        _fits(row_token.dtype == _value_dtypes["int32"] and row_token.numel() >= n_rows and row_token.is_contiguous(),
               "row_token: a dense int32 for every row of q")
     _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
                                     _stream(stream)), "moe_quantize_rows")
@@ -271,7 +284,7 @@ def moe_quantize_weights(w, q, scale, stream=None):
     """w [E, n_out, n_in] (bf16 or fp32) into the 8-bit weights q, scale (see fp8_weight_buffers)."""
     dtype = _value_dtype(w, 3, "w")
     e, n_out, n_in = w.shape
-    pitch, scale_pitch = moe_fp8_query(n_in)
+    pitch, scale_pitch = _fp8_pitches(n_in)
     blocks = -(-n_out // 128)
     _fits_fp8(q, (e, blocks * 128, pitch), "q")
     _fits_fp8(scale, (e, blocks, scale_pitch), "scale")

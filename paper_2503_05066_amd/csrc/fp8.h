@@ -124,7 +124,7 @@ struct Fp8Args {
     int experts;
     int pitch, scale_pitch;            // of x and of a weight row
     int n, n_pad, y_scale_pitch;
-    int col_group;
+    int col_group, tile_shift;
     int stream;                        // the weights' lines need not be kept
 };
 // One launch over all tiles; the shape: 256 weight rows, gate and up rows of 128 columns or not, or 128.

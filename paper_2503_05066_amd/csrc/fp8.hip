@@ -554,7 +554,7 @@ __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w,
 // The order of the work, found by every wave for itself from the experts' offsets: no launch ahead of this one builds a
 // schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
 //
-// First the full row tiles (256 rows), expert by expert, then what is left of the experts' rows, higher tiles first, so that the
+// First the full row tiles (256 rows, or 128 or 64: see launch_fp8_shape), expert by expert, then what is left of the experts' rows, higher tiles first, so that the
 // last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the XCDs in turn (block id mod 8), and the
 // blocks of an XCD take the items of its chunks in turn.  About as many tiles as an expert has make a chunk: those that run
 // together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
@@ -565,11 +565,11 @@ struct TileOrder {
     const int32_t* offset;
     int ends[kChunks];  // of expert 64 c + lane: full tiles up to and including its own
     uint32_t parts;     // of place 64 c + lane among the partly filled tiles: its expert, in byte c
-    int full, tiles, slabs, n_pad, group, deal, row_chunks, chunks;
+    int sh, full, tiles, slabs, n_pad, group, deal, row_chunks, chunks;  // 1 << sh: rows of a full tile
     bool stream;
 
     __device__ __forceinline__ TileOrder(const Fp8Args& p, int lane, uint8_t* scratch)
-        : offset(p.expert_offset), slabs(p.pitch / kFp8Block), n_pad(p.n_pad), group(p.col_group), stream(p.stream) {
+        : offset(p.expert_offset), sh(p.tile_shift), slabs(p.pitch / kFp8Block), n_pad(p.n_pad), group(p.col_group), stream(p.stream) {
         int rows[kChunks];
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
@@ -581,7 +581,7 @@ struct TileOrder {
         int active = 0;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
-            int n = rows[c] >> 8;
+            int n = rows[c] >> sh;
 #pragma unroll
             for (int off = 1; off < kWave; off <<= 1) {
                 const int o = __shfl_up(n, off, kWave);
@@ -599,7 +599,7 @@ struct TileOrder {
         for (int height = 8; height > 0; --height)
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-                const bool mine = ((rows[c] & 255) + 31) >> 5 == height;
+                const bool mine = ((rows[c] & ((1 << sh) - 1)) + 31) >> 5 == height;
                 const uint64_t all = __ballot(mine);
                 if (mine) *word(n_parts + __popcll(all & below)) = c * kWave + lane;
                 n_parts += __popcll(all);
@@ -648,10 +648,10 @@ struct TileOrder {
         w.valid = 1;
         w.e = e;
         w.n0 = col * S::kNCols;
-        w.row0 = whole ? lo + (tile - before) * S::BM : lo + ((hi - lo) & ~(S::BM - 1));
-        w.rows = whole ? S::BM : (hi - lo) & (S::BM - 1);
+        w.row0 = whole ? lo + ((tile - before) << sh) : lo + ((hi - lo) >> sh << sh);
+        w.rows = whole ? 1 << sh : (hi - lo) & ((1 << sh) - 1);
         // an expert's only tile, in a layer whose weights the memory-side cache does not keep (see ffn.hip)
-        w.once = stream && hi - lo <= S::BM;
+        w.once = stream && hi - lo <= 1 << sh;
         w.first = 0;
         w.slabs = slabs;
         w.turn = w.once ? (int)((long long)w.n0 * slabs / n_pad) : 0;
@@ -769,10 +769,15 @@ void launch_fp8_shape(Fp8Args p, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
     });
     const int nb = p.n_pad / S::kNCols;
-    // a block per compute unit, the same number on every XCD; fewer where the plan cannot hold as many items
-    const int per_xcd = std::max(1, compute_units() / 8);
-    const long long items = nb * ((long long)(p.max_rows / kFfnTileM) + std::min<long long>(p.max_rows, p.experts));
-    const int grid = 8 * (int)std::min<long long>(per_xcd, (items + 7) / 8);
+    const long long active = std::min<long long>(p.max_rows, p.experts);
+    // Lower row tiles as long as their items still fit one round of the chip's 256 compute units (the bound counts a partly
+    // filled tile of every expert).  Tiles of 64, 128, 256 rows: one expert, 203 rows of 2056 x 5640 12.4, 15.0, 18.2 us, 512 rows
+    // 20.3, 16.4, 20.1, 1024 28.7, 26.3, 22.1; the FFN of one expert of 4096 x 2048, 512 tokens 46.5, 56.9, 78.1, 2048 92.6, 75.0,
+    // 91.6, 4096 151, 122, 111; of 8 experts of 2048 x 1024 with 1024 rows 43.6, 42.6, 53.4, with 2048 60.3, 51.9, 55.5.
+    p.tile_shift = 8;
+    while (p.tile_shift > 6 && nb * ((p.max_rows >> (p.tile_shift - 1)) + active) <= 256 + 32) --p.tile_shift;
+    // a block per compute unit, the same number on every XCD (which of them get items is known on the device only)
+    const int grid = 8 * std::max(1, compute_units() / 8);
     p.col_group = nb % 4 == 0 ? 4 : (nb % 3 == 0 ? 3 : (nb % 2 == 0 ? 2 : 1));
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(S::kThreads), S::kLdsBytes, st, p);
 }

@@ -1,9 +1,10 @@
 // Products on 8-bit expert weights for experts of few rows (fp8.hip has the others): decoding steps and any batch with a
 // small capacity.
 //
-// The work is streaming weights.  A block has 32 weight rows: 32 output columns, or the gate and up rows of 16 hidden
-// columns.  Its four waves split K and share nothing until the end: each keeps a ring of its own in LDS, filled by direct
-// loads, waits for its own slabs only and needs no barrier (as the bf16 kernel, ffn_thin.hip).  Two blocks share a compute unit.
+// The work is streaming weights.  A wave has 32 weight rows: 32 output columns, or the gate and up rows of 16 hidden
+// columns.  The four waves of a block take different rows or parts of K (see thin_split) and share nothing until the end: each
+// keeps a ring of its own in LDS, filled by direct loads, waits for its own slabs only and needs no barrier (as the bf16 kernel,
+// ffn_thin.hip).  Two blocks share a compute unit.
 //
 // bf16 activations are quantised as they leave LDS: every block does it for itself, 130 vector instructions for 16 rows of a
 // slab beside 4 KB of weights, which take twice as long to arrive; kernels of their own for it, one ahead of either product,
@@ -17,8 +18,8 @@ namespace capmoe {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
-constexpr int kThin8WeightRows = 32;         // weight rows of a block
-constexpr int kThin8Waves = 4;               // waves of a block; each multiplies a quarter of K
+constexpr int kThin8WeightRows = 32;         // weight rows of a wave
+constexpr int kThin8Waves = 4;               // waves of a block
 constexpr int kThin8RingBytes = 20 * 1024;   // LDS of a wave
 
 struct Thin8Args {
@@ -31,9 +32,10 @@ struct Thin8Args {
     const uint8_t* w_scale[2];
     uint16_t* y;
     int experts, k, pitch, n, n_pad, scale_pitch, col_blocks;
+    int split;            // waves that share a row of weights, each with a part of K: 4, 2 or 1
 };
 
-// One pass: up to NR rows of an expert times a block's weight rows.
+// One pass: up to NR rows of an expert times a block's weight rows, of which those of its first wave begin at n0.
 // QUANT: x is bf16.  ONCE: the weights' lines need not be kept.
 template <int NR, bool SWIGLU, bool QUANT, bool ONCE>
 struct Thin8 {
@@ -52,8 +54,10 @@ struct Thin8 {
         asm volatile("" : "+v"(tid));  // what follows from it is computed here, not for all shapes at the block's start
         const int lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int lr = lane & 15, lk = lane >> 4;
+        n0 += wv / p.split * kCols;
         const int slabs_all = p.pitch / kFp8Block;
-        const int first = wv * slabs_all / kThin8Waves, n = (wv + 1) * slabs_all / kThin8Waves - first;
+        const int part = wv & (p.split - 1);  // of K
+        const int first = part * slabs_all / p.split, n = n0 < p.n_pad ? (part + 1) * slabs_all / p.split - first : 0;
         // column blocks start their walks at different slabs: in step they would all read at the same offset of a
         // power-of-two pitch, i.e. from a few memory channels (see ffn.hip)
         const int turn = (int)((int64_t)n0 * n / p.n_pad);
@@ -216,27 +220,28 @@ struct Thin8 {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        // ---- the four partial tiles meet in LDS (every wave in its own ring) and are added in wave order ----
-        f32x4* mine = (f32x4*)ring;
-        if (wv > 0) {
+        // ---- partial tiles meet in LDS (every wave in its own ring) and are added in wave order ----
+        if (p.split > 1) {
+            f32x4* mine = (f32x4*)ring;
+            if (part > 0) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int m = 0; m < TM; ++m) mine[(q * TM + m) * 64 + lane] = acc[q][m];
-        }
-        __syncthreads();
-        if (wv > 0) return;
+                    for (int m = 0; m < TM; ++m) mine[(q * TM + m) * 64 + lane] = acc[q][m];
+            }
+            __syncthreads();
+            if (part > 0) return;
+            for (int u = 1; u < p.split; ++u) {
+                const f32x4* other = (const f32x4*)(ring + u * kThin8RingBytes);
 #pragma unroll
-        for (int u = 1; u < kThin8Waves; ++u) {
-            const f32x4* part = (const f32x4*)(smem + u * kThin8RingBytes);
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+                    for (int m = 0; m < TM; ++m) {
+                        const f32x4 o = other[(q * TM + m) * 64 + lane];
 #pragma unroll
-                for (int m = 0; m < TM; ++m) {
-                    const f32x4 o = part[(q * TM + m) * 64 + lane];
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[q][m][v] += o[v];
-                }
+                        for (int v = 0; v < 4; ++v) acc[q][m][v] += o[v];
+                    }
+            }
         }
 #pragma unroll
         for (int m = 0; m < TM; ++m) {
@@ -304,11 +309,11 @@ __global__ __launch_bounds__(64 * kThin8Waves, 2) void fp8_thin_kernel(const Thi
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     constexpr int kMost = QUANT ? 16 : 32;  // rows of a pass
     ExpertRows x(p.expert_offset, p.experts);
-    const int first = blockIdx.x / p.col_blocks, n0 = (blockIdx.x - first * p.col_blocks) * Thin8<16, SWIGLU, QUANT, STREAM>::kCols;
+    const int first = blockIdx.x / p.col_blocks, n0 = (blockIdx.x - first * p.col_blocks) * (kThin8Waves / p.split) * Thin8<16, SWIGLU, QUANT, STREAM>::kCols;
     const int step = gridDim.x / p.col_blocks;
     for (int t = first; x.find(t); t += step) {
         for (int at = 0; at < x.rows; at += kMost) {
-            if (t > first || at > 0) __syncthreads();  // the first wave reads the others' sums out of their rings
+            if (t > first || at > 0) __syncthreads();  // a wave may still read the others' sums out of their rings
             if (x.rows > kMost)
                 Thin8<kMost, SWIGLU, QUANT, false>::run(p, x.e, x.row0 + at, min(x.rows - at, kMost), n0, smem);
             else if (QUANT && x.rows <= 4)
@@ -321,6 +326,15 @@ __global__ __launch_bounds__(64 * kThin8Waves, 2) void fp8_thin_kernel(const Thi
     }
 }
 
+// How many waves share a weight row.  2048 waves fill the chip; whole rows keep a wave's ring full for longer, shorter parts
+// end sooner.  Products at 4, 2, 1: one token's 8 experts of 64 x 2048 x 1024 (512 waves with whole rows) FFN 18.6, 19.4, 24.9 us;
+// two tokens' (960) 32.7, 27.0, 27.2; four tokens' (2048) 58, 48, 41; 16 tokens', 108, 86, 75; 64 x 4096 x 1408 (5632) 227, 190, 185;
+// 8 experts of 14336 columns by 4096 (1024, but long) 73.4, 77.0, 76.4.
+static int thin_split(int64_t waves, int slabs) {
+    if (waves <= 512 || (waves <= 1024 && slabs >= 64)) return 4;
+    return waves <= 1024 ? 2 : 1;
+}
+
 template <bool SWIGLU, bool QUANT, bool STREAM>
 static void launch_thin8(Thin8Args a, int64_t tiles, hipStream_t st) {
     constexpr int lds = kThin8Waves * kThin8RingBytes;
@@ -330,7 +344,9 @@ static void launch_thin8(Thin8Args a, int64_t tiles, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     });
     constexpr int cols = Thin8<16, SWIGLU, QUANT, STREAM>::kCols;
-    a.col_blocks = (a.n + cols - 1) / cols;
+    a.split = thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kFp8Block);
+    const int per_block = kThin8Waves / a.split * cols;
+    a.col_blocks = (a.n + per_block - 1) / per_block;
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * a.col_blocks)), dim3(64 * kThin8Waves), lds, st, a);
 }
 
