@@ -259,7 +259,7 @@ int moe_fp8_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch);
 /*
  * Rows of activations to 8 bits, on the way permuted if row_token is given (moe_dispatch and quantising in one pass):
  * q[r,:], scale[r,:] from x[row_token ? row_token[r] : r, :] for r < n_rows, and r < *row_count if that is given
- * (device; expert_offset + E holds the rows of a plan).  Rows behind stay untouched.
+ * (device; expert_offset + E holds the rows of a plan).  Rows behind stay untouched.  row_token holds rows of x (not checked).
  *   dtype MOE_DTYPE_* of x [*,cols]; rows are moved in 16-byte pieces: cols a multiple of 8 (bf16) or 4 (fp32),
  *   x and q 16-byte aligned, scale 4-byte aligned.
  * n_rows == 0 enqueues nothing, and its arrays may be null.  Fewer than 2^31 blocks of 128, else MOE_ERR_UNSUPPORTED.
@@ -267,14 +267,15 @@ int moe_fp8_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch);
 int moe_quantize_rows(int dtype, const void* x, int64_t n_rows, int32_t cols, const int32_t* row_token,
                       const int32_t* row_count, void* q, uint8_t* scale, void* stream);
 
-/* Expert weights w [n_experts, n_out, n_in] in dtype to 8 bits, padding included.  n_in as `cols` above. */
+/* Expert weights w [n_experts, n_out, n_in] in dtype to 8 bits, padding included.  n_in as `cols` above; n_out at most 2^21;
+ * fewer than 2^24 blocks of 128 x 128, else MOE_ERR_UNSUPPORTED. */
 int moe_quantize_weights(int dtype, const void* w, int32_t n_experts, int32_t n_out, int32_t n_in, void* q,
                          uint8_t* scale, void* stream);
 
 /* One product of 8-bit rows and 8-bit expert weights (host memory, plain data). */
 typedef struct {
     int32_t max_rows;   /* most rows of y: expert_offset[E] <= max_rows                                        */
-    int32_t src_rows;   /* rows of x when they are fetched through row_token; ignored without a row_token      */
+    int32_t src_rows;   /* rows of x when they are fetched through row_token (then not 0); ignored without one  */
     int32_t n_experts;  /* E, at most 256                                                                      */
     int32_t n_in;       /* columns of x and of a weight row, at most 2^21                                      */
     int32_t n_out;      /* columns of y and rows of an expert's weights: a multiple of 8, at most 2^21         */
@@ -288,7 +289,7 @@ int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes);
  *   y[r,n] = sum_k x[row_token ? row_token[r] : r, k] * w[e,n,k]          y [max_rows,n_out] bf16
  * of the values that x (8-bit rows) and w (8-bit weights) stand for, accumulated in fp32 on the matrix cores, rounded once.
  * Offsets are ascending from 0 (device); an expert may have no rows.  Rows at or behind expert_offset[E] stay untouched.
- * n_experts = 1 is a plain product (an expert that all tokens share).  With row_token, x must be smaller than 4 GiB, else
+ * n_experts = 1 is a plain product (an expert that all tokens share).  With row_token, src_rows * pitch < 2^32 - 15, else
  * MOE_ERR_UNSUPPORTED.  The same call gives the same bits; the order of a row's sums may differ with the number of rows
  * of its expert and of the batch.  y must be 16-byte aligned.
  */
@@ -313,8 +314,11 @@ int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes);
  * moe_grouped_ffn, moe_dispatch_ffn and moe_layer_forward with 8-bit experts.  desc->dtype is MOE_DTYPE_BF16 (the type of
  * xp / x, yp and y); any other is MOE_ERR_UNSUPPORTED.  d is a multiple of 8, h any number; d and h at most 2^21.  The
  * activations are quantised on the way: xp / x by rows, and the hidden activation, rounded to bf16 once, by rows too.
- * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp8 and moe_layer_forward_fp8: N * d < 2^31.
- * Under a profile table the quantising of x counts as MOE_KERNEL_DISPATCH.
+ * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp8 and moe_layer_forward_fp8: N * d < 2^31 and
+ * N * pitch(d) < 2^32 - 15; all three: P_max * ceil(max(d, h) / 128) < 2^31; else MOE_ERR_UNSUPPORTED.  Where no row can
+ * survive (P_max = 0) nothing is enqueued for the FFN, and x, xp, row_token and yp may be null.
+ * Batches of few rows per expert quantise x and the hidden activation inside the products, with the same result;
+ * where the quantising of x is a launch of its own, a profile table counts it as MOE_KERNEL_DISPATCH.
  */
 int moe_grouped_ffn_fp8(const moe_desc_t* desc, const void* xp, const int32_t* expert_offset,
                         const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,

@@ -46,8 +46,15 @@ static int validate_fp8(const moe_desc_t* d) {
     const int v = validate(d);
     if (v != MOE_OK) return v;
     if (d->dtype != MOE_DTYPE_BF16 || d->d_model > kFp8MaxWidth || d->d_hidden > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
-    if (derive(*d).max_rows >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
+    const int64_t rows = derive(*d).max_rows, blocks = fp8_blocks(std::max(d->d_model, d->d_hidden));
+    if (rows >= (int64_t)1 << 31 || rows * blocks >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
     return MOE_OK;
+}
+
+// The first product addresses all of x, as bf16 or as 8-bit rows, through one window of 4 GiB.
+static bool too_large_to_gather(const moe_desc_t* d) {
+    return (uint64_t)d->n_tokens * (uint64_t)d->d_model >= (1ull << 31) ||
+           (uint64_t)d->n_tokens * (uint64_t)fp8_pitch(d->d_model) > kBeyond;
 }
 
 static int validate_experts(const moe_fp8_experts_t* w) {
@@ -151,16 +158,16 @@ static int ffn_fp8_impl(const moe_desc_t* desc, const void* x, const int32_t* ro
                : MOE_ERR_HIP;
 }
 
-static int ffn_fp8_checked(const moe_desc_t* desc, const void* x, const int32_t* row_token, const int32_t* expert_offset,
+static int ffn_fp8_checked(const moe_desc_t* desc, const void* x, bool gathered, const int32_t* row_token, const int32_t* expert_offset,
                            const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes, void* stream) {
     const int v = validate_fp8(desc);
     if (v != MOE_OK) return v;
-    if (!x || !expert_offset || !yp || !workspace) return MOE_ERR_INVALID_ARG;
+    const Sizes s = derive(*desc);
+    if (!expert_offset || !workspace || (s.max_rows > 0 && (!x || !yp || (gathered && !row_token)))) return MOE_ERR_INVALID_ARG;
     if (misaligned16(x) || misaligned16(yp) || ((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
     const int w = validate_experts(experts);
     if (w != MOE_OK) return w;
-    if (row_token && (uint64_t)desc->n_tokens * (uint64_t)desc->d_model >= (1ull << 31)) return MOE_ERR_UNSUPPORTED;
-    const Sizes s = derive(*desc);
+    if (gathered && too_large_to_gather(desc)) return MOE_ERR_UNSUPPORTED;
     const Fp8Workspace ws = ffn_fp8_workspace(*desc, s, workspace);
     if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
     if (s.max_rows == 0) return MOE_OK;
@@ -203,7 +210,7 @@ int moe_quantize_weights(int dtype, const void* w, int32_t n_experts, int32_t n_
     if (n_experts < 1 || n_out < 1) return MOE_ERR_INVALID_ARG;
     if (n_out > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
     if (!w || !q || !scale || misaligned16(w) || misaligned16(q) || misaligned4(scale)) return MOE_ERR_INVALID_ARG;
-    if ((int64_t)fp8_blocks(n_out) * fp8_blocks(n_in) >= ((int64_t)1 << 31) / n_experts) return MOE_ERR_UNSUPPORTED;
+    if ((int64_t)fp8_blocks(n_out) * fp8_blocks(n_in) >= ((int64_t)1 << 24) / n_experts) return MOE_ERR_UNSUPPORTED;  // blocks of a launch
     return launch_quantize_weights(dtype, w, n_experts, n_out, n_in, q, scale, (hipStream_t)stream) == hipSuccess ? MOE_OK
                                                                                                                    : MOE_ERR_HIP;
 }
@@ -224,6 +231,7 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (misaligned16(x) || misaligned16(w) || misaligned16(y) || misaligned4(x_scale) || misaligned4(w_scale)) return MOE_ERR_INVALID_ARG;
     (void)workspace, (void)workspace_bytes;  // none is needed
     const Fp8Gemm g = fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
+    if (row_token && gemm->max_rows > 0 && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
     if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -253,14 +261,13 @@ int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes) {
 int moe_grouped_ffn_fp8(const moe_desc_t* desc, const void* xp, const int32_t* expert_offset,
                         const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
                         void* stream) {
-    return ffn_fp8_checked(desc, xp, nullptr, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+    return ffn_fp8_checked(desc, xp, false, nullptr, expert_offset, experts, yp, workspace, workspace_bytes, stream);
 }
 
 int moe_dispatch_ffn_fp8(const moe_desc_t* desc, const void* x, const int32_t* expert_offset, const int32_t* row_token,
                          const moe_fp8_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
                          void* stream) {
-    if (!row_token) return MOE_ERR_INVALID_ARG;
-    return ffn_fp8_checked(desc, x, row_token, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+    return ffn_fp8_checked(desc, x, true, row_token, expert_offset, experts, yp, workspace, workspace_bytes, stream);
 }
 
 int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_router, const float* bias,
@@ -280,7 +287,7 @@ int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_
         if (misaligned16(x) || misaligned16(w_router) || misaligned16(yp) || misaligned16(y) || misaligned16(scores) ||
             misaligned16(topk_idx) || misaligned16(pair_row))
             return MOE_ERR_INVALID_ARG;
-        if ((uint64_t)desc->n_tokens * (uint64_t)desc->d_model >= (1ull << 31)) return MOE_ERR_UNSUPPORTED;
+        if (too_large_to_gather(desc)) return MOE_ERR_UNSUPPORTED;
     }
     if (s.max_rows > 0) {
         if (!row_token) return MOE_ERR_INVALID_ARG;

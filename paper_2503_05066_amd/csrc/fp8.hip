@@ -84,8 +84,9 @@ struct Fills8 {
     }
     __device__ __forceinline__ void aim(const WorkItem& w, const Fp8Args& p, int lane, int wm, int wn) {
         const int32_t* gather = p.gather;
-        a = __builtin_amdgcn_make_buffer_rsrc((void*)(gather ? p.x : p.x + (size_t)w.row0 * p.pitch), 0, -1, kRsrcFlags);
         const int64_t x0 = gather ? 0 : w.row0;
+        a = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x + x0 * p.pitch), 0,
+                                              (int)(uint32_t)min((p.x_rows - x0) * p.pitch, (int64_t)kBeyond), kRsrcFlags);
         sa = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x_scale + x0 * p.scale_pitch), 0,
                                                (int)(uint32_t)min((p.x_rows - x0) * p.scale_pitch, (int64_t)kBeyond), kRsrcFlags);
         const size_t n_at = (size_t)w.e * p.n_pad + w.n0;
@@ -512,7 +513,7 @@ __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w,
                 float o[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    o[k] = g[k] * u[k] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g[k] * -1.4426950408889634f));
+                    o[k] = g[k] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g[k] * -1.4426950408889634f)) * u[k];
                 v[j][2 * i] = pack_bf16x2(o[0], o[1]);
                 v[j][2 * i + 1] = pack_bf16x2(o[2], o[3]);
             });
@@ -554,8 +555,8 @@ __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w,
 // The order of the work, found by every wave for itself from the experts' offsets: no launch ahead of this one builds a
 // schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
 //
-// First the full row tiles (256 rows, or 128 or 64: see launch_fp8_shape), expert by expert, then what is left of the experts' rows, higher tiles first, so that the
-// last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the XCDs in turn (block id mod 8), and the
+// First the full row tiles (256 rows, or 128 or 64: see launch_fp8_shape), expert by expert, then what is left of the experts'
+// rows, higher tiles first, so that the last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the XCDs in turn (block id mod 8), and the
 // blocks of an XCD take the items of its chunks in turn.  About as many tiles as an expert has make a chunk: those that run
 // together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
 // (A ticket per item instead of turns: the same within 2 % where all items are alike, and counters that somebody has to clear.)

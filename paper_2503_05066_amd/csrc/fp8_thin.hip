@@ -6,8 +6,8 @@
 // keeps a ring of its own in LDS, filled by direct loads, waits for its own slabs only and needs no barrier (as the bf16 kernel,
 // ffn_thin.hip).  Two blocks share a compute unit.
 //
-// bf16 activations are quantised as they leave LDS: every block does it for itself, 130 vector instructions for 16 rows of a
-// slab beside 4 KB of weights, which take twice as long to arrive; kernels of their own for it, one ahead of either product,
+// bf16 activations are quantised as they leave LDS: every block does it for itself, for up to 16 rows of a
+// slab beside 4 KB of weights, which take longer to arrive; kernels of their own for it, one ahead of either product,
 // would cost their launches.  Nor is there a tile schedule: a block finds its expert in the offsets.
 #include <algorithm>
 
@@ -54,10 +54,10 @@ struct Thin8 {
         asm volatile("" : "+v"(tid));  // what follows from it is computed here, not for all shapes at the block's start
         const int lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int lr = lane & 15, lk = lane >> 4;
-        n0 += wv / p.split * kCols;
+        n0 += wv / p.split * kCols;  // below n_pad: a block's columns divide 128
         const int slabs_all = p.pitch / kFp8Block;
         const int part = wv & (p.split - 1);  // of K
-        const int first = part * slabs_all / p.split, n = n0 < p.n_pad ? (part + 1) * slabs_all / p.split - first : 0;
+        const int first = part * slabs_all / p.split, n = (part + 1) * slabs_all / p.split - first;
         // column blocks start their walks at different slabs: in step they would all read at the same offset of a
         // power-of-two pitch, i.e. from a few memory channels (see ffn.hip)
         const int turn = (int)((int64_t)n0 * n / p.n_pad);
@@ -254,7 +254,7 @@ struct Thin8 {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     const float g = acc[0][m][v];
-                    o[v] = g * acc[1][m][v] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
+                    o[v] = g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * acc[1][m][v];
                 }
                 if (col < p.n) *(uint2*)out = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
             } else {

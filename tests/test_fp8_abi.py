@@ -70,7 +70,7 @@ def test_quantize_weights_refusals():
 
     assert call(dtype=7) == INVALID and call(e=0) == INVALID and call(n=0) == INVALID and call(k=0) == INVALID
     assert call(k=12) == UNSUPPORTED and call(dtype=0, k=3) == UNSUPPORTED and call(n=(1 << 21) + 1) == UNSUPPORTED
-    assert call(e=1 << 10, n=1 << 21, k=1 << 21) == UNSUPPORTED
+    assert call(e=1 << 10, n=1 << 21, k=1 << 21) == UNSUPPORTED and call(e=1 << 12, n=1 << 13, k=1 << 13) == UNSUPPORTED
     for a in ("w", "q", "s"):
         assert call(**{a: None}) == INVALID
     assert call(w=P + 4) == INVALID and call(q=P + 1) == INVALID and call(s=P + 1) == INVALID
@@ -86,7 +86,7 @@ def test_gemm_refusals():
         return lib.moe_grouped_gemm_fp8(ctypes.byref(g), a["x"], a["xs"], a["token"], a["off"], a["w"], a["ws"], a["y"],
                                         a["work"], a["size"], None)
 
-    for bad in (dict(rows=-1), dict(src=-1), dict(e=0), dict(k=0), dict(n=0)):
+    for bad in (dict(rows=-1), dict(src=-1), dict(e=0), dict(k=0), dict(n=0), dict(token=P, src=0)):
         assert call(**bad) == INVALID
     for bad in (dict(e=257), dict(n=12), dict(n=(1 << 21) + 8), dict(k=(1 << 21) + 1), dict(token=P, src=1 << 20, k=1 << 13)):
         assert call(**bad) == UNSUPPORTED
@@ -138,6 +138,13 @@ def test_ffn_refusals():
         assert f(desc=_desc(gamma=0.0)) == OK  # no row can survive
     assert fused(token=None) == INVALID
     assert fused(desc=_desc(n_tokens=1 << 17, d_model=1 << 14)) == UNSUPPORTED
+    # d fills 16 bytes a row of x, but 128 of its 8-bit form
+    narrow = dict(n_tokens=1 << 25, d_model=8, n_experts=4, top_k=1, gamma=0.001)
+    assert fused(desc=_desc(**narrow)) == UNSUPPORTED
+    # more blocks of 128 than the quantising counts
+    assert grouped(desc=_desc(n_tokens=1 << 20, d_model=1 << 15, top_k=8, mode=capmoe.MODE_NONE)) == UNSUPPORTED
+    none = _desc(gamma=0.0)
+    assert grouped(desc=none, x=None, yp=None) == OK and fused(desc=none, x=None, token=None, yp=None) == OK
     assert lib.moe_grouped_ffn_fp8(ctypes.byref(_desc()), P, P, None, P, P, 1 << 40, None) == INVALID
 
 
@@ -158,6 +165,7 @@ def test_layer_refusals():
     for n in ("scores", "topk_idx", "pair_row", "yp", "y", "workspace"):
         assert call(**{n: P + 4}) == INVALID, n
     assert call(experts=_experts(down=None)) == INVALID
+    assert call(desc=_desc(n_tokens=1 << 25, d_model=8, n_experts=4, top_k=1, gamma=0.001)) == UNSUPPORTED
     need = capmoe.moe_query_fp8(_desc())
     assert call(size=need - 1) == SMALL and need >= capmoe.moe_query(_desc())[3]
 

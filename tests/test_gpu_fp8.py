@@ -166,6 +166,28 @@ def test_product_through_a_plan(counts, k, n):
     p.check(p.run())
 
 
+# Room for more rows than there are makes the row tiles higher (a rule on max_rows): 128 and 256 rows, here with every height in
+# steps of 32; n: the narrow and the wide shape
+@pytest.mark.parametrize("k", [8, 128, 256, 384, 512, 640, 896, 1032, 1152, 2048])
+@pytest.mark.parametrize("n,room", [(120, 20000), (264, 13000), (128, 40000), (392, 40000), (256, 60000), (512, 60000)])
+def test_product_on_high_tiles(k, n, room):
+    p = Product([1, 33, 70, 100, 0, 130, 161, 200, 230, 261, 768, 250], k, n)
+    y = p.run(extra=room)
+    assert torch.all(y[p.rows:] == 7.0)
+    p.check(y)
+
+
+@pytest.mark.parametrize("e,k,n,most", [(40, 520, 512, 8), (70, 136, 512, 8), (30, 1416, 1000, 16), (90, 256, 392, 40), (33, 8, 1032, 3)])
+def test_product_of_many_experts_of_few_rows(e, k, n, most):
+    # two and one of a block's waves share a weight row; more than one pass over an expert's weights
+    g = rng(e, most)
+    counts = g.integers(0, most + 1, e)
+    if most > 16:
+        counts[counts < 33] = 0
+    p = Product(list(counts), k, n)
+    p.check(p.run(extra=3))
+
+
 @pytest.mark.parametrize("e,k,n", [(256, 256, 264), (130, 136, 512), (65, 384, 1024)])
 def test_product_of_many_experts(e, k, n):
     g = rng(e)
@@ -246,7 +268,8 @@ def plan_of(g, tokens, counts):
 
 FFN = [(1, 256, 8, 2, 128, [1, 0, 0, 0, 0, 0, 0, 1]), (16, 512, 4, 2, 384, [16, 0, 7, 9]), (37, 264, 6, 2, 200, [37, 1, 0, 20, 16, 0]),
        (300, 256, 4, 2, 384, [300, 2, 0, 290]), (520, 1032, 3, 2, 136, [520, 64, 300]), (700, 384, 5, 2, 1416, [257, 700, 100, 0, 33]),
-       (5, 136, 2, 1, 8, [2, 3]), (1000, 512, 8, 4, 640, [1000, 700, 512, 256, 255, 96, 0, 130])]
+       (5, 136, 2, 1, 8, [2, 3]), (64, 264, 64, 2, 384, [2, 0, 1, 5] * 16), (40, 392, 40, 2, 264, [1, 4, 0, 2, 0] * 8),
+       (90, 256, 1, 1, 384, [90]), (30, 640, 1, 1, 128, [29]), (12, 256, 256, 6, 128, [0, 1, 0, 0] * 64), (1000, 512, 8, 4, 640, [1000, 700, 512, 256, 255, 96, 0, 130])]
 
 
 @pytest.mark.parametrize("tokens,d,e,k,h,counts", FFN)
@@ -280,6 +303,41 @@ def test_ffn(tokens, d, e, k, h, counts):
     assert torch.equal(yp, yp2)
 
 
+@pytest.mark.parametrize("tokens,d,k,h", [(5000, 136, 4, 128), (14000, 256, 4, 128), (14000, 136, 4, 264), (6000, 1032, 4, 384), (10000, 640, 4, 512)])
+def test_ffn_on_high_tiles(tokens, d, k, h):
+    counts = [1, 33, 70, 100, 0, 130, 161, 200, 230, 261, 768, 250]
+    desc, x, weights, _, _ = layer(tokens, d, len(counts), k, h, mode=capmoe.MODE_NONE)
+    offset, token = plan_of(rng(2, tokens), tokens, counts)
+    rows = len(token)
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xA5)
+    yp = torch.full((tokens * k, d), 7.0, dtype=BF16, device="cuda")
+    padded = np.zeros(tokens * k, np.int32)
+    padded[:rows] = token
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(padded), experts, yp, ws)
+    assert torch.all(yp[rows:] == 7.0)
+    values = [ref.weights_value(*ref.quantize_weights(plain(w))) for w in weights]
+    want = ref.ffn(plain(x)[token], *values, offset)[:, :d]
+    off = plain(yp[:rows]) - want
+    assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want), np.linalg.norm(off) / np.linalg.norm(want)
+    rms = np.sqrt(np.mean(want ** 2))
+    assert np.abs(off).max() <= 0.5 * np.maximum(rms, np.abs(want).max() / 8)
+
+
+@pytest.mark.parametrize("tokens", [4, 300])
+def test_gates_that_are_shut(tokens):
+    # gate -2^71 and up 2^71: their product leaves the range of fp32, silu(gate) * up is a zero
+    desc, x, weights, _, _ = layer(tokens, 128, 2, 1, 128, mode=capmoe.MODE_NONE)
+    x.fill_(2.0 ** 64)
+    weights[0].fill_(-1.0), weights[1].fill_(1.0), weights[2].fill_(1.0)
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    yp = torch.full((tokens, 128), 7.0, dtype=BF16, device="cuda")
+    capmoe.moe_grouped_ffn_fp8(desc, x, on(np.array([0, tokens // 2, tokens], np.int32)), experts, yp, ws)
+    assert torch.all(yp == 0)
+
+
 def test_a_token_that_is_not_a_number_stays_by_itself():
     desc, x, weights, _, _ = layer(400, 256, 4, 1, 384, mode=capmoe.MODE_NONE)
     x[7, 3], x[200, 255] = float("nan"), float("inf")
@@ -295,10 +353,38 @@ def test_a_token_that_is_not_a_number_stays_by_itself():
     assert set(np.flatnonzero(bad)) == {200, 305}
 
 
+@pytest.mark.parametrize("tokens,counts", [(12, [12, 3, 0, 9]), (300, [300, 64, 0, 211])])
+def test_tokens_of_zeros_and_of_extreme_sizes(tokens, counts):
+    desc, x, weights, _, _ = layer(tokens, 264, 4, 3, 200, mode=capmoe.MODE_NONE)
+    x[1], x[2] = 0, 0
+    x[3] *= 2.0 ** -100
+    x[4] *= 2.0 ** 60  # the hidden activation reaches 2^120
+    x[5, :128] = 0     # a block of zeros beside another
+    x[6] = 1e-40       # below the type's normal numbers
+    offset, token = plan_of(rng(5, tokens), tokens, counts)
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    yp = torch.zeros((capmoe.moe_query(desc)[2], 264), dtype=BF16, device="cuda")
+    padded = np.zeros(yp.shape[0], np.int32)
+    padded[:len(token)] = token
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(padded), experts, yp, ws)
+    got = plain(yp)[:len(token)]
+    values = [ref.weights_value(*ref.quantize_weights(plain(w))) for w in weights]
+    want = ref.ffn(plain(x), *values, offset, token)[:, :264]
+    assert np.all(got[np.isin(token, (1, 2))] == 0)
+    assert np.all(np.abs(got[np.isin(token, (3, 6))]) <= 2.0 ** -90)
+    rest = ~np.isin(token, (1, 2, 3, 6))
+    err = np.linalg.norm(got[rest] - want[rest], axis=1) / np.linalg.norm(want[rest], axis=1)
+    # a row's own error: one value in 2^10 of its 200 on the other side of a border is one at most, of 2^-3 * three times the mean
+    # square of 200: 2^-5.2, and the two roundings
+    assert np.all(err <= 2.0 ** -5), err.max()
+
+
 LAYERS = [dict(tokens=64, d=256, e=8, k=2, h=384, device_groups=4, mode=capmoe.MODE_EXPANDED_DROP),
           dict(tokens=512, d=512, e=16, k=4, h=640, mode=capmoe.MODE_TOKEN_DROP, gamma=1.5),
           dict(tokens=1, d=264, e=8, k=2, h=200, mode=capmoe.MODE_NONE),
           dict(tokens=300, d=256, e=4, k=1, h=128, mode=capmoe.MODE_TOKEN_DROP, gamma=0.0),
+          dict(tokens=0, d=256, e=4, k=2, h=128, mode=capmoe.MODE_TOKEN_DROP),
           dict(tokens=2048, d=256, e=8, k=2, h=256, mode=capmoe.MODE_TOKEN_DROP, capacity_scope=capmoe.SCOPE_GLOBAL)]
 
 
