@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* __restri
 }
 
 // A block of 256 threads takes a 128 x 128 block of an expert's weights and keeps it in registers: 16 lanes to a row,
-// eight rows a thread.
+// eight rows a thread.  64 x 1024 x 2048 in bf16 76 us, 5.3 TB/s (a copy of 1 GiB 4.7).
 template <bool BF16>
 __global__ __launch_bounds__(256) void quantize_weights_kernel(const void* __restrict__ w, uint8_t* __restrict__ q,
                                                                uint8_t* __restrict__ scale, int n_out, int n_in, int n_blocks,
@@ -151,7 +151,9 @@ hipError_t launch_quantize_rows(int dtype, const void* x, int64_t n_rows, int co
                                 const int32_t* row_count, void* q, uint8_t* scale, hipStream_t st) {
     const Divisor blocks((uint32_t)fp8_blocks(cols));
     const int64_t groups = n_rows * blocks.d;
-    const dim3 grid((unsigned)std::min<int64_t>((groups + 15) / 16, 256 * 64));
+    // (8192 x 4096 bf16: 18.6 us with up to 16384 blocks, 16.3, 6.2 TB/s, with 4096; fp32 29.0 and 30.2; two or four blocks of values
+    // requested at once are no faster)
+    const dim3 grid((unsigned)std::min<int64_t>((groups + 15) / 16, dtype == MOE_DTYPE_BF16 ? 4096 : 16384));
     auto kern = dtype == MOE_DTYPE_BF16 ? quantize_rows_kernel<true> : quantize_rows_kernel<false>;
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, x, row_token, row_count, (uint8_t*)q, scale, n_rows, cols, fp8_scale_pitch(cols),
                        blocks);
