@@ -552,6 +552,18 @@ __device__ __forceinline__ int write_hidden(const Fp8Args& p, const WorkItem& w,
     return 2 * live;
 }
 
+// The sum of the lanes' values up to and including the lane's own.  (By shuffles through LDS, four scans of six one after the other:
+// a launch's first request 4.1 instead of 3.5 us behind its start.)
+__device__ __forceinline__ int sum_up_to(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr: in rows of 16 lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15: a row's last lane to the next row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
+    return v;
+}
+
 // The order of the work, found by every wave for itself from the experts' offsets: no launch ahead of this one builds a
 // schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
 //
@@ -582,13 +594,7 @@ struct TileOrder {
         int active = 0;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
-            int n = rows[c] >> sh;
-#pragma unroll
-            for (int off = 1; off < kWave; off <<= 1) {
-                const int o = __shfl_up(n, off, kWave);
-                n += lane >= off ? o : 0;
-            }
-            ends[c] = full + n;
+            ends[c] = full + sum_up_to(rows[c] >> sh);
             full = __builtin_amdgcn_readlane(ends[c], kWave - 1);
             active += __popcll(__ballot(rows[c] > 0));
         }
@@ -600,6 +606,7 @@ struct TileOrder {
         for (int height = 8; height > 0; --height)
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
+                if (c * kWave >= p.experts) continue;
                 const bool mine = ((rows[c] & ((1 << sh) - 1)) + 31) >> 5 == height;
                 const uint64_t all = __ballot(mine);
                 if (mine) *word(n_parts + __popcll(all & below)) = c * kWave + lane;
@@ -608,6 +615,7 @@ struct TileOrder {
         parts = 0;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) parts |= ((uint32_t)*word(c * kWave + lane) & 255u) << (8 * c);
+        n_parts = __builtin_amdgcn_readfirstlane(n_parts);  // behind the branches the compiler would take it for a lane's own
         tiles = full + n_parts;
         const int columns = n_pad / S::kNCols;
         const int each = tiles / max(active, 1);  // tiles of an expert, on average

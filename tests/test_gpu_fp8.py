@@ -458,3 +458,48 @@ def test_the_same_call_gives_the_same_bits():
     first = p.run()
     for _ in range(3):
         assert torch.equal(first, p.run())
+
+
+@pytest.mark.parametrize("counts,most", [([3, 0, 7, 2], 4096), ([300, 0, 200, 12], 4096), ([1, 0, 4, 2], 12)])
+def test_captured_product_follows_its_offsets(counts, most):
+    # the grid depends on max_rows alone: a replay does the plan that its arrays then hold
+    k, n = 520, 392
+    p = Product([most // 4] * 4, k, n)
+    y = torch.zeros((most, n), dtype=BF16, device="cuda")
+    x, xs, off, w, ws = (on(a) for a in (p.xq, p.xs, p.offset, p.wq, p.ws))
+    gemm = capmoe.make_gemm(most, k, n, 4)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    capmoe.moe_grouped_gemm_fp8(gemm, x, xs, None, off, w, ws, y, none)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        capmoe.moe_grouped_gemm_fp8(gemm, x, xs, None, off, w, ws, y, none)
+    for now in (counts, [most // 4] * 4, counts[::-1], [0, 0, 0, 0], [most, 0, 0, 0]):
+        p.offset = np.concatenate([[0], np.cumsum(now)]).astype(np.int32)
+        p.rows = int(p.offset[-1])
+        off.copy_(torch.from_numpy(p.offset))
+        y.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.all(y[p.rows:] == 7.0)
+        p.check(y)
+
+
+def test_calls_on_two_streams_at_once():
+    cases = [layer(**LAYERS[i], seed=9) for i in (0, 1, 5)]
+    experts = [capmoe.Fp8Experts.quantized(*c[2]) for c in cases]
+    want = []
+    for (desc, x, _, w_router, bias), e in zip(cases, experts):
+        buf = capmoe.LayerBuffers(desc, fp8=True)
+        capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, e, None, 0, buf)
+        want.append(buf)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [capmoe.LayerBuffers(c[0], fp8=True) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (desc, x, _, w_router, bias), e, buf, stream in zip(cases, experts, got, streams):
+            capmoe.moe_layer_forward_fp8(desc, x, w_router, bias, e, None, 0, buf, stream=stream)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.y, b.y) and torch.equal(a.expert_offset, b.expert_offset)
