@@ -568,9 +568,18 @@ __device__ __forceinline__ int sum_up_to(int v) {
 // schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
 //
 // First the full row tiles (256 rows, or 128 or 64: see launch_fp8_shape), expert by expert, then what is left of the experts'
-// rows, higher tiles first, so that the last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the XCDs in turn (block id mod 8), and the
-// blocks of an XCD take the items of its chunks in turn.  About as many tiles as an expert has make a chunk: those that run
-// together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
+// rows, higher tiles first, so that the last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the
+// XCDs in turn (block id mod 8), and the blocks of an XCD take the items of its chunks in turn.  About as many tiles as an
+// expert has make a chunk: those that run together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
+// Which chunk follows: with few rounds of items (up to 4.5 a block) the next column group of the same tiles, so that the heights
+// fall all along, and every other round, of a block's turns and of the XCDs', runs backwards: who had the higher tile of one gets
+// the lower of the next.  With more rounds the next tiles of the same column group: the heights fall once per column group, and low
+// tiles, which wait for weights, run beside high ones.  The latter and the former order, us: products of 3000 tokens on
+// 64 x 2048 x 1024 (1.3 rounds) 55.8, 48.2; 4096 on 32 x 4096 x 2048 (1.4) 130, 112; 9000 top-1 on 8 x 1024 x 4096 (1.8) 46.6, 50.0; 6000 on
+// 8 x 4096 x 4096 (2.2) 146, 137; 12413 on 60 x 512 x 1280 (4.3) 77, 71; 8192 on 64 x 2048 x 2048 (4.6) 164, 165; 3000 on 32 x 4096 x 8192 (5.3) 304, 340;
+// FFN of 3000 tokens on 8 x 4096 x 4096 (2.4) 275, 246; 4096 on 64 x 2048 x 1024 (2.7) 172, 171 to 176; 6500 (4.1) 266, 254; 8192 on
+// 32 x 2048 x 2048 (5.0) 285, 298; 12413 on 60 x 512 x 1280 (8.6) 210, 218.
+//
 // (A ticket per item instead of turns: the same within 2 % where all items are alike, and counters that somebody has to clear.)
 template <class S>
 struct TileOrder {
@@ -578,8 +587,8 @@ struct TileOrder {
     const int32_t* offset;
     int ends[kChunks];  // of expert 64 c + lane: full tiles up to and including its own
     uint32_t parts;     // of place 64 c + lane among the partly filled tiles: its expert, in byte c
-    int sh, full, tiles, slabs, n_pad, group, deal, row_chunks, chunks;  // 1 << sh: rows of a full tile
-    bool stream;
+    int sh, full, tiles, slabs, n_pad, group, deal, inner, chunks;  // 1 << sh: rows of a full tile
+    bool stream, few_rounds;
 
     __device__ __forceinline__ TileOrder(const Fp8Args& p, int lane, uint8_t* scratch)
         : offset(p.expert_offset), sh(p.tile_shift), slabs(p.pitch / kFp8Block), n_pad(p.n_pad), group(p.col_group), stream(p.stream) {
@@ -624,8 +633,10 @@ struct TileOrder {
         // a chunk (FFN of 1531 tokens on 60 x 2048 x 1408, eleven column blocks: 127 -> 120 us; where experts have two, 4096 on
         // 64 x 2048 x 1024, it would be 176 -> 191).
         if (tiles == active && tiles >= 4 * 8) group = columns;
-        row_chunks = (tiles + deal - 1) / deal;
-        chunks = row_chunks * (columns / group);
+        const int row_chunks = (tiles + deal - 1) / deal, col_groups = columns / group;
+        chunks = row_chunks * col_groups;
+        few_rounds = 2 * tiles * columns <= 9 * (int)gridDim.x;
+        inner = few_rounds ? col_groups : row_chunks;
     }
     // position p of this XCD's share; past its end: not valid, `more` false; a place that the last chunk of a column group
     // leaves empty: not valid, `more` true
@@ -633,11 +644,12 @@ struct TileOrder {
         WorkItem w;
         w.valid = 0;
         const int per_chunk = deal * group, j = p / per_chunk, in = p - j * per_chunk;
-        const int chunk = xcd + 8 * j;
+        const int chunk = 8 * j + (few_rounds && (j & 1) ? 7 - xcd : xcd);
         more = chunk < chunks;
         if (!more) return w;
-        const int cg = chunk / row_chunks, tr = in / group;
-        int tile = (chunk - cg * row_chunks) * deal + tr, col = cg * group + in - tr * group;
+        const int first = chunk / inner, rest = chunk - first * inner;
+        const int cg = few_rounds ? rest : first, tr = in / group;
+        int tile = (few_rounds ? first : rest) * deal + tr, col = cg * group + in - tr * group;
         tile = __builtin_amdgcn_readfirstlane(tile), col = __builtin_amdgcn_readfirstlane(col);
         if (tile >= tiles) return w;
         const bool whole = tile < full;
@@ -666,13 +678,13 @@ struct TileOrder {
         w.turn = w.once ? (int)((long long)w.n0 * slabs / n_pad) : 0;
         return w;
     }
-    // the item at place p or the next one of the same block behind it
-    __device__ __forceinline__ WorkItem next(int xcd, int& p, int step) const {
+    // the item of block `turn` of an XCD's `blocks` in this round, or the next one that it has
+    __device__ __forceinline__ WorkItem next(int xcd, int& round, int turn, int blocks) const {
         bool more = true;
         WorkItem w;
         do {
-            w = at(xcd, p, more);
-            p += step;
+            w = at(xcd, round * blocks + (few_rounds && (round & 1) ? blocks - 1 - turn : turn), more);
+            ++round;
         } while (more && !w.valid);
         return w;
     }
@@ -691,8 +703,9 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
     const int wm = wv >> 1, wn = wv & 1;
     const int per_xcd = gridDim.x >> 3, xcd = blockIdx.x & 7;
     const TileOrder<S> order(p, lane, smem + wv * (kMaxExperts * 4));
-    int place = blockIdx.x >> 3;
-    WorkItem cur = order.next(xcd, place, per_xcd);
+    const int turn = blockIdx.x >> 3;
+    int round = 0;
+    WorkItem cur = order.next(xcd, round, turn, per_xcd);
     if (!cur.valid) return;
     __syncthreads();  // the waves' scratch
     const int lr = lane & 15, lk = lane >> 4;
@@ -746,7 +759,7 @@ __global__ __launch_bounds__(S::kThreads) void fp8_gemm_kernel(const Fp8Args p) 
             loop(std::true_type{});
         else
             loop(std::false_type{});
-        const WorkItem nxt = order.next(xcd, place, per_xcd);
+        const WorkItem nxt = order.next(xcd, round, turn, per_xcd);
         younger = 0;
         if (nxt.valid) {
             fills.aim(nxt, p, lane, wm, wn);

@@ -177,6 +177,15 @@ def test_product_on_high_tiles(k, n, room):
     p.check(y)
 
 
+@pytest.mark.parametrize("counts,k,n", [([300, 0, 70], 8, 102400), ([520, 30, 260, 600], 136, 39432)])
+def test_product_of_many_rounds(counts, k, n):
+    # more than 4.5 items for every compute unit: another order of the work
+    p = Product(counts, k, n)
+    y = p.run(extra=1)
+    assert torch.all(y[p.rows:] == 7.0)
+    p.check(y)
+
+
 @pytest.mark.parametrize("e,k,n,most", [(40, 520, 512, 8), (70, 136, 512, 8), (30, 1416, 1000, 16), (90, 256, 392, 40), (33, 8, 1032, 3)])
 def test_product_of_many_experts_of_few_rows(e, k, n, most):
     # two and one of a block's waves share a weight row; more than one pass over an expert's weights
@@ -266,7 +275,7 @@ def plan_of(g, tokens, counts):
     return offset, token
 
 
-FFN = [(1, 256, 8, 2, 128, [1, 0, 0, 0, 0, 0, 0, 1]), (16, 512, 4, 2, 384, [16, 0, 7, 9]), (37, 264, 6, 2, 200, [37, 1, 0, 20, 16, 0]),
+FFN = [(300, 136, 2, 2, 51200, [300, 40]), (1, 256, 8, 2, 128, [1, 0, 0, 0, 0, 0, 0, 1]), (16, 512, 4, 2, 384, [16, 0, 7, 9]), (37, 264, 6, 2, 200, [37, 1, 0, 20, 16, 0]),
        (300, 256, 4, 2, 384, [300, 2, 0, 290]), (520, 1032, 3, 2, 136, [520, 64, 300]), (700, 384, 5, 2, 1416, [257, 700, 100, 0, 33]),
        (5, 136, 2, 1, 8, [2, 3]), (64, 264, 64, 2, 384, [2, 0, 1, 5] * 16), (40, 392, 40, 2, 264, [1, 4, 0, 2, 0] * 8),
        (90, 256, 1, 1, 384, [90]), (30, 640, 1, 1, 128, [29]), (12, 256, 256, 6, 128, [0, 1, 0, 0] * 64), (1000, 512, 8, 4, 640, [1000, 700, 512, 256, 255, 96, 0, 130])]
