@@ -315,8 +315,21 @@ class Fp8Experts:
     """The 8-bit weights of a layer's experts (keeps the tensors alive; allocation and marshalling only)."""
 
     def __init__(self, gate, gate_scale, up, up_scale, down, down_scale):
+        e, h, d = gate.shape
+        for q, scale, n, k in ((gate, gate_scale, h, d), (up, up_scale, h, d), (down, down_scale, d, h)):
+            if tuple(q.shape) != (e, n, k) or n % 128 or k % 128 or q.element_size() != 1 or not q.is_contiguous():
+                raise ValueError(f"8-bit expert weights {tuple(q.shape)}: expected {(e, n, k)}, multiples of 128, one byte, contiguous")
+            if tuple(scale.shape) != (e, n // 128, -(-k // 512) * 4) or scale.element_size() != 1 or not scale.is_contiguous():
+                raise ValueError(f"scales {tuple(scale.shape)} of expert weights {(e, n, k)}")
+        self.sizes = (e, h, d)  # filled up to multiples of 128
         self.tensors = (gate, gate_scale, up, up_scale, down, down_scale)
         self.struct = MoeFp8Experts(*[t.data_ptr() for t in self.tensors])
+
+    def of(self, desc: MoeDesc):
+        """The struct for a call of that layer."""
+        if self.sizes != (desc.n_experts, -(-desc.d_hidden // 128) * 128, -(-desc.d_model // 128) * 128):
+            raise ValueError(f"8-bit experts of {self.sizes} do not belong to this layer")
+        return ctypes.byref(self.struct)
 
     @classmethod
     def quantized(cls, w_gate, w_up, w_down, stream=None):
@@ -355,14 +368,14 @@ def moe_query_fp8(desc: MoeDesc) -> int:
 
 
 def moe_grouped_ffn_fp8(desc, xp, expert_offset, experts: Fp8Experts, yp, workspace, stream=None):
-    _check(load().moe_grouped_ffn_fp8(ctypes.byref(desc), _ptr(xp), _ptr(expert_offset), ctypes.byref(experts.struct),
+    _check(load().moe_grouped_ffn_fp8(ctypes.byref(desc), _ptr(xp), _ptr(expert_offset), experts.of(desc),
                                       _ptr(yp), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                       _stream(stream)), "moe_grouped_ffn_fp8")
 
 
 def moe_dispatch_ffn_fp8(desc, x, expert_offset, row_token, experts: Fp8Experts, yp, workspace, stream=None):
     _check(load().moe_dispatch_ffn_fp8(ctypes.byref(desc), _ptr(x), _ptr(expert_offset), _ptr(row_token),
-                                       ctypes.byref(experts.struct), _ptr(yp), _ptr(workspace),
+                                       experts.of(desc), _ptr(yp), _ptr(workspace),
                                        workspace.numel() * workspace.element_size(), _stream(stream)),
            "moe_dispatch_ffn_fp8")
 
@@ -371,7 +384,7 @@ def moe_layer_forward_fp8(desc, x, w_router, bias, experts: Fp8Experts, token_cl
     """The whole layer with 8-bit experts, into the buffers of a LayerBuffers made with fp8=True."""
     ws = buf.workspace
     _check(load().moe_layer_forward_fp8(
-        ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(bias), ctypes.byref(experts.struct), _ptr(token_class),
+        ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(bias), experts.of(desc), _ptr(token_class),
         int(seed) & 0xFFFFFFFF, _ptr(buf.logits), _ptr(buf.scores), _ptr(buf.topk_idx), _ptr(buf.topk_score),
         _ptr(buf.expert_count), _ptr(buf.seg_count), _ptr(buf.expert_offset), _ptr(buf.row_token),
         _ptr(buf.row_weight), _ptr(buf.pair_row), _ptr(buf.yp), _ptr(buf.y), _ptr(ws),

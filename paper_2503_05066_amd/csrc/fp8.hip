@@ -678,7 +678,7 @@ struct TileOrder {
         w.turn = w.once ? (int)((long long)w.n0 * slabs / n_pad) : 0;
         return w;
     }
-    // the item of block `turn` of an XCD's `blocks` in this round, or the next one that it has
+    // the item that block `turn` of an XCD's `blocks` takes in its round `round`, or the next one that it has
     __device__ __forceinline__ WorkItem next(int xcd, int& round, int turn, int blocks) const {
         bool more = true;
         WorkItem w;
@@ -793,9 +793,10 @@ void launch_fp8_shape(Fp8Args p, hipStream_t st) {
     const int nb = p.n_pad / S::kNCols;
     const long long active = std::min<long long>(p.max_rows, p.experts);
     // Lower row tiles as long as their items still fit one round of the chip's 256 compute units (the bound counts a partly
-    // filled tile of every expert).  Tiles of 64, 128, 256 rows: one expert, 203 rows of 2056 x 5640 12.4, 15.0, 18.2 us, 512 rows
-    // 20.3, 16.4, 20.1, 1024 28.7, 26.3, 22.1; the FFN of one expert of 4096 x 2048, 512 tokens 46.5, 56.9, 78.1, 2048 92.6, 75.0,
-    // 91.6, 4096 151, 122, 111; of 8 experts of 2048 x 1024 with 1024 rows 43.6, 42.6, 53.4, with 2048 60.3, 51.9, 55.5.
+    // filled tile of every expert).  Tiles of 64, 128, 256 rows, us: one expert, 203 rows of 2056 x 5640 11.8, 14.4, 17.6, 512 rows
+    // 20.0, 15.7, 19.5, 1024 29.5, 26.9, 23.6; the FFN of one expert of 4096 x 2048, 512 tokens 45.5, 54.9, 77.1, 2048 95.6, 82.3, 96.0 (its
+    // products take different ones: 73.5), 4096 162, 131, 112; 512 tokens top-2 on 8 experts of 2048 x 1024 34.1, 39.4, 38.5, 1024 45.9, 42.8,
+    // 55.7, 2048 62.2, 56.1, 60.4 (taken: 35.5, 46.6, 60.2); 1500 on 8 of 4096 x 4096 247, 202, 168.
     p.tile_shift = 8;
     while (p.tile_shift > 6 && nb * ((p.max_rows >> (p.tile_shift - 1)) + active) <= 256 + 32) --p.tile_shift;
     // a block per compute unit, the same number on every XCD (which of them get items is known on the device only)

@@ -192,3 +192,25 @@ def test_binding_refuses_tensors_that_do_not_fit():
                 lambda: capmoe.moe_quantize_weights(w.transpose(0, 1), q, s), lambda: capmoe.moe_quantize_weights(w[0], q, s)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_experts_that_do_not_fit_are_refused():
+    def made(e=2, h=200, d=72, **change):
+        sizes = {"gate": (e, h, d), "up": (e, h, d), "down": (e, d, h), **change}
+        parts = [t for n in ("gate", "up", "down") for t in capmoe.fp8_weight_buffers(*sizes[n], device="cpu")]
+        return capmoe.Fp8Experts(*parts)
+
+    good = made()
+    assert good.sizes == (2, 256, 128)
+    for bad in (dict(up=(2, 300, 72)), dict(up=(3, 200, 72)), dict(down=(2, 200, 72)), dict(down=(2, 72, 300)), dict(down=(1, 72, 200))):
+        with pytest.raises(ValueError):
+            made(**bad)
+    t = list(good.tensors)
+    for i, bad in ((0, t[0][:, :, :64]), (1, t[1][:, :1]), (4, t[4].transpose(1, 2)), (5, t[5].int()), (2, t[2].short())):
+        with pytest.raises(ValueError):
+            capmoe.Fp8Experts(*t[:i], bad, *t[i + 1:])
+    x = torch.zeros((16, 72), dtype=torch.bfloat16)
+    for desc in (_desc(d_model=72, n_experts=3), _desc(d_model=136, n_experts=2), _desc(d_model=72, n_experts=2, d_hidden=257)):
+        for call in (lambda: capmoe.moe_grouped_ffn_fp8(desc, x, None, good, x, x), lambda: capmoe.moe_dispatch_ffn_fp8(desc, x, None, None, good, x, x)):
+            with pytest.raises(ValueError):
+                call()
