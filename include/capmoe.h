@@ -291,7 +291,7 @@ int moe_gemm_query(const moe_gemm_t* gemm, size_t* workspace_bytes);
  * Offsets are ascending from 0 (device); an expert may have no rows.  Rows at or behind expert_offset[E] stay untouched.
  * n_experts = 1 is a plain product (an expert that all tokens share).  With row_token, src_rows * pitch < 2^32 - 15, else
  * MOE_ERR_UNSUPPORTED.  The same call gives the same bits; the order of a row's sums may differ with the number of rows
- * of its expert and of the batch.  y must be 16-byte aligned.
+ * of its expert and of the batch.  y must be 16-byte aligned.  max_rows == 0 enqueues nothing, and its arrays may be null.
  */
 int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x_scale, const int32_t* row_token,
                          const int32_t* expert_offset, const void* w, const uint8_t* w_scale, void* y, void* workspace,

@@ -227,13 +227,13 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
                          size_t workspace_bytes, void* stream) {
     const int v = validate_gemm(gemm);
     if (v != MOE_OK) return v;
+    if (gemm->max_rows == 0) return MOE_OK;
     if (!x || !x_scale || !expert_offset || !w || !w_scale || !y) return MOE_ERR_INVALID_ARG;
     if (misaligned16(x) || misaligned16(w) || misaligned16(y) || misaligned4(x_scale) || misaligned4(w_scale)) return MOE_ERR_INVALID_ARG;
     (void)workspace, (void)workspace_bytes;  // none is needed
     const Fp8Gemm g = fp8_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
-    if (row_token && gemm->max_rows > 0 && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
+    if (row_token && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
-    if (gemm->max_rows == 0) return MOE_OK;
     hipStream_t st = (hipStream_t)stream;
     const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
     const bool streamed = weights_stream((double)g.experts * g.pitch * g.n_pad);

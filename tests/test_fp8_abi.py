@@ -96,6 +96,7 @@ def test_gemm_refusals():
         assert call(**{a: P + 8}) == INVALID
     assert call(xs=P + 2) == INVALID and call(ws=P + 1) == INVALID
     assert call(rows=0) == OK  # nothing to do, nothing launched
+    assert call(rows=0, **{a: None for a in ("x", "xs", "off", "w", "ws", "y")}) == OK  # tensors of no rows have no address
     assert capmoe.moe_gemm_query(capmoe.make_gemm(8, 256, 64, 4)) == 0 and call(rows=0, work=None, size=0) == OK
     assert lib.moe_grouped_gemm_fp8(None, P, P, None, P, P, P, P, P, 1 << 30, None) == INVALID
     assert lib.moe_gemm_query(None, None) == INVALID
