@@ -354,10 +354,11 @@ def moe_gemm_query(gemm: MoeGemm) -> int:
 
 
 def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace, stream=None):
+    """workspace may be None where moe_gemm_query answers 0."""
     _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), _ptr(x), _ptr(x_scale), _ptr(row_token), _ptr(expert_offset),
                                        _ptr(w), _ptr(w_scale), _ptr(y), _ptr(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream(stream)),
-           "moe_grouped_gemm_fp8")
+                                       workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                       _stream(stream)), "moe_grouped_gemm_fp8")
 
 
 def moe_query_fp8(desc: MoeDesc) -> int:

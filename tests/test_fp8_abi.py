@@ -215,3 +215,18 @@ def test_experts_that_do_not_fit_are_refused():
         for call in (lambda: capmoe.moe_grouped_ffn_fp8(desc, x, None, good, x, x), lambda: capmoe.moe_dispatch_ffn_fp8(desc, x, None, None, good, x, x)):
             with pytest.raises(ValueError):
                 call()
+
+
+class _NoStream:
+    """A stream for calls that must be over before anything is enqueued on it."""
+
+    cuda_stream = None
+    device_index = 0
+
+
+def test_binding_passes_no_workspace_to_a_product():
+    gemm = capmoe.make_gemm(0, 256, 64, 2)
+    xq, xs = capmoe.fp8_row_buffers(0, 256, device="cpu")
+    wq, ws = capmoe.fp8_weight_buffers(2, 64, 256, device="cpu")
+    y, offset = torch.zeros((0, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    capmoe.moe_grouped_gemm_fp8(gemm, xq, xs, None, offset, wq, ws, y, None, stream=_NoStream)
