@@ -242,6 +242,13 @@ def _fits(ok, what):
         raise ValueError(what)
 
 
+@functools.lru_cache(maxsize=None)
+def _dtype(name):
+    import torch
+
+    return getattr(torch, name)
+
+
 _value_dtypes = {}
 
 
@@ -353,8 +360,42 @@ def moe_gemm_query(gemm: MoeGemm) -> int:
     return ws.value
 
 
+@functools.lru_cache(maxsize=256)
+def _product_shapes(gemm: bytes):
+    """The fields of a MoeGemm that the call accepts, and what they say of the tensors."""
+    sizes = MoeGemm.from_buffer_copy(gemm)
+    moe_gemm_query(sizes)  # refuses sizes that the call refuses
+    pitch, scale_pitch = moe_fp8_query(sizes.n_in)
+    e, blocks = sizes.n_experts, -(-sizes.n_out // 128)
+    return sizes.max_rows, sizes.src_rows, e, sizes.n_out, pitch, scale_pitch, (e, blocks * 128, pitch), (e, blocks, scale_pitch)
+
+
+def _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
+    """Every tensor against the sizes of the call.  (Of rows that are not gathered, x holds as many as expert_offset ends with,
+    which is known on the device only.)"""
+    max_rows, src_rows, e, n_out, pitch, scale_pitch, w_shape, w_scale_shape = _product_shapes(bytes(gemm))
+    if max_rows == 0:
+        return
+    for t in (x, x_scale, expert_offset, w, w_scale, y):
+        if t is None or not t.is_contiguous():
+            raise ValueError("a product of rows takes dense tensors x, x_scale, expert_offset, w, w_scale and y")
+    shape = x.shape
+    rows = shape[0] if shape else 0
+    _fits(shape == (rows, pitch) and x.element_size() == 1, "x: bytes [rows, pitch]")
+    _fits(x_scale.shape == (rows, scale_pitch) and x_scale.element_size() == 1, "x_scale: bytes [rows of x, scale_pitch]")
+    _fits(w.shape == w_shape and w.element_size() == 1, "w: bytes [E, n_out and n_in filled up to multiples of 128]")
+    _fits(w_scale.shape == w_scale_shape and w_scale.element_size() == 1, "w_scale: bytes [E, blocks of n_out, scale_pitch]")
+    shape = y.shape
+    _fits(len(shape) == 2 and shape[1] == n_out and shape[0] >= max_rows and y.dtype == _dtype("bfloat16"), "y: bf16 [max_rows, n_out]")
+    _fits(expert_offset.dtype == _dtype("int32") and expert_offset.numel() > e, "expert_offset: int32 [E + 1]")
+    if row_token is not None:
+        _fits(rows >= src_rows, "x: src_rows rows")
+        _fits(row_token.dtype == _dtype("int32") and row_token.numel() >= max_rows and row_token.is_contiguous(), "row_token: a dense int32 [max_rows]")
+
+
 def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace, stream=None):
-    """workspace may be None where moe_gemm_query answers 0."""
+    """workspace may be None where moe_gemm_query answers 0.  A tensor that does not fit the sizes of gemm is refused."""
+    _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y)
     _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), _ptr(x), _ptr(x_scale), _ptr(row_token), _ptr(expert_offset),
                                        _ptr(w), _ptr(w_scale), _ptr(y), _ptr(workspace),
                                        workspace.numel() * workspace.element_size() if workspace is not None else 0,

@@ -230,3 +230,45 @@ def test_binding_passes_no_workspace_to_a_product():
     wq, ws = capmoe.fp8_weight_buffers(2, 64, 256, device="cpu")
     y, offset = torch.zeros((0, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
     capmoe.moe_grouped_gemm_fp8(gemm, xq, xs, None, offset, wq, ws, y, None, stream=_NoStream)
+
+
+def _product(rows=6, e=2, k=264, n=200, src=0):
+    """Arguments of a product that belong together, on the host."""
+    a = dict(gemm=capmoe.make_gemm(rows, k, n, e, src_rows=src), row_token=None, workspace=None)
+    a["x"], a["x_scale"] = capmoe.fp8_row_buffers(src or rows, k, device="cpu")
+    a["w"], a["w_scale"] = capmoe.fp8_weight_buffers(e, n, k, device="cpu")
+    a["y"], a["expert_offset"] = torch.zeros((rows, n), dtype=torch.bfloat16), torch.zeros(e + 1, dtype=torch.int32)
+    if src:
+        a["row_token"] = torch.zeros(rows, dtype=torch.int32)
+    return a
+
+
+def test_binding_refuses_tensors_that_do_not_fit_a_product():
+    def refused(**change):
+        with pytest.raises(ValueError):
+            capmoe.moe_grouped_gemm_fp8(**{**a, **change}, stream=_NoStream)
+
+    a = _product(src=4)
+    refused(x=a["x"][:, :256]), refused(x=a["x"].short()), refused(x=a["x"].T), refused(x=a["x"][0]), refused(x=a["x"].repeat(1, 2)[:, ::2])
+    refused(x=a["x"][:3], x_scale=a["x_scale"][:3])  # fewer rows than the plan's tokens
+    refused(x_scale=a["x_scale"][:3]), refused(x_scale=a["x_scale"].int()), refused(x_scale=a["x_scale"].repeat(1, 2))
+    refused(w=a["w"][:, :200]), refused(w=a["w"][:1]), refused(w=a["w"][:, :, :264]), refused(w=a["w"].transpose(1, 2)), refused(w=a["w"].bfloat16())
+    refused(w_scale=a["w_scale"][:, :1]), refused(w_scale=a["w_scale"].float()), refused(w_scale=a["w_scale"][0])
+    refused(y=a["y"][:5]), refused(y=a["y"][:, :192]), refused(y=a["y"].float()), refused(y=a["y"].half()), refused(y=a["y"].T), refused(y=a["y"][0])
+    refused(y=torch.zeros((6, 400), dtype=torch.bfloat16)[:, ::2])
+    refused(expert_offset=a["expert_offset"][:2]), refused(expert_offset=a["expert_offset"].long())
+    refused(expert_offset=torch.zeros(6, dtype=torch.int32)[::2])
+    refused(row_token=a["row_token"][:5]), refused(row_token=a["row_token"].long()), refused(row_token=torch.zeros(12, dtype=torch.int32)[::2])
+    for name in ("x", "x_scale", "expert_offset", "w", "w_scale", "y"):
+        refused(**{name: None})
+    a = _product()
+    refused(x=a["x"][:, :256]), refused(x_scale=a["x_scale"][:5])
+
+
+def test_product_without_rows_takes_no_tensors():
+    a = _product(rows=0)
+    capmoe.moe_grouped_gemm_fp8(a["gemm"], None, None, None, None, None, None, None, None, stream=_NoStream)
+    for bad in (capmoe.make_gemm(-1, 256, 64), capmoe.make_gemm(4, 0, 64), capmoe.make_gemm(4, 256, 0), capmoe.make_gemm(4, 256, 64, 0),
+                capmoe.make_gemm(4, 256, 12), capmoe.make_gemm(4, 256, 64, 257), capmoe.make_gemm(4, (1 << 21) + 8, 64)):
+        with pytest.raises(capmoe.CapMoeError):  # the call's own refusals
+            capmoe.moe_grouped_gemm_fp8(bad, **{k: v for k, v in a.items() if k != "gemm"}, stream=_NoStream)
