@@ -150,6 +150,20 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _stream_on(stream, *tensors):
+    """_stream for calls that look at their tensors: all of them lie on the stream's device (host memory, or another GPU's, is
+    no address of a kernel there)."""
+    if stream is None:
+        import torch
+
+        stream = torch.cuda.current_stream()
+    device = stream.device_index
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor on {t.device}, a stream of device {device}")
+    return stream.cuda_stream
+
+
 def _check(status: int, what: str):
     if status != MOE_OK:
         raise CapMoeError(status, what)
@@ -284,7 +298,7 @@ def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
         _fits(row_token.dtype == _value_dtypes["int32"] and row_token.numel() >= n_rows and row_token.is_contiguous(),
               "row_token: a dense int32 for every row of q")
     _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
-                                    _stream(stream)), "moe_quantize_rows")
+                                    _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows")
 
 
 def moe_quantize_weights(w, q, scale, stream=None):
@@ -295,7 +309,7 @@ def moe_quantize_weights(w, q, scale, stream=None):
     blocks = -(-n_out // 128)
     _fits_fp8(q, (e, blocks * 128, pitch), "q")
     _fits_fp8(scale, (e, blocks, scale_pitch), "scale")
-    _check(load().moe_quantize_weights(dtype, _ptr(w), e, n_out, n_in, _ptr(q), _ptr(scale), _stream(stream)),
+    _check(load().moe_quantize_weights(dtype, _ptr(w), e, n_out, n_in, _ptr(q), _ptr(scale), _stream_on(stream, w, q, scale)),
            "moe_quantize_weights")
 
 
@@ -328,6 +342,8 @@ class Fp8Experts:
                 raise ValueError(f"8-bit expert weights {tuple(q.shape)}: expected {(e, n, k)}, multiples of 128, one byte, contiguous")
             if tuple(scale.shape) != (e, n // 128, -(-k // 512) * 4) or scale.element_size() != 1 or not scale.is_contiguous():
                 raise ValueError(f"scales {tuple(scale.shape)} of expert weights {(e, n, k)}")
+            if q.device != gate.device or scale.device != gate.device:
+                raise ValueError("8-bit expert weights on more than one device")
         self.sizes = (e, h, d)  # filled up to multiples of 128
         self.tensors = (gate, gate_scale, up, up_scale, down, down_scale)
         self.struct = MoeFp8Experts(*[t.data_ptr() for t in self.tensors])
@@ -399,7 +415,8 @@ def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale,
     _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), _ptr(x), _ptr(x_scale), _ptr(row_token), _ptr(expert_offset),
                                        _ptr(w), _ptr(w_scale), _ptr(y), _ptr(workspace),
                                        workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                       _stream(stream)), "moe_grouped_gemm_fp8")
+                                       _stream_on(stream, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace)),
+           "moe_grouped_gemm_fp8")
 
 
 def moe_query_fp8(desc: MoeDesc) -> int:
@@ -412,13 +429,14 @@ def moe_query_fp8(desc: MoeDesc) -> int:
 def moe_grouped_ffn_fp8(desc, xp, expert_offset, experts: Fp8Experts, yp, workspace, stream=None):
     _check(load().moe_grouped_ffn_fp8(ctypes.byref(desc), _ptr(xp), _ptr(expert_offset), experts.of(desc),
                                       _ptr(yp), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                      _stream(stream)), "moe_grouped_ffn_fp8")
+                                      _stream_on(stream, xp, expert_offset, yp, workspace, experts.tensors[0])), "moe_grouped_ffn_fp8")
 
 
 def moe_dispatch_ffn_fp8(desc, x, expert_offset, row_token, experts: Fp8Experts, yp, workspace, stream=None):
     _check(load().moe_dispatch_ffn_fp8(ctypes.byref(desc), _ptr(x), _ptr(expert_offset), _ptr(row_token),
                                        experts.of(desc), _ptr(yp), _ptr(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream(stream)),
+                                       workspace.numel() * workspace.element_size(),
+                                       _stream_on(stream, x, expert_offset, row_token, yp, workspace, experts.tensors[0])),
            "moe_dispatch_ffn_fp8")
 
 
@@ -430,7 +448,8 @@ def moe_layer_forward_fp8(desc, x, w_router, bias, experts: Fp8Experts, token_cl
         int(seed) & 0xFFFFFFFF, _ptr(buf.logits), _ptr(buf.scores), _ptr(buf.topk_idx), _ptr(buf.topk_score),
         _ptr(buf.expert_count), _ptr(buf.seg_count), _ptr(buf.expert_offset), _ptr(buf.row_token),
         _ptr(buf.row_weight), _ptr(buf.pair_row), _ptr(buf.yp), _ptr(buf.y), _ptr(ws),
-        ws.numel() * ws.element_size(), _stream(stream)), "moe_layer_forward_fp8")
+        ws.numel() * ws.element_size(), _stream_on(stream, x, w_router, bias, token_class, ws, experts.tensors[0])),
+        "moe_layer_forward_fp8")
     return buf.y
 
 

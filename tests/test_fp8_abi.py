@@ -221,7 +221,7 @@ class _NoStream:
     """A stream for calls that must be over before anything is enqueued on it."""
 
     cuda_stream = None
-    device_index = 0
+    device_index = -1  # that of tensors in host memory
 
 
 def test_binding_passes_no_workspace_to_a_product():
@@ -272,3 +272,42 @@ def test_product_without_rows_takes_no_tensors():
                 capmoe.make_gemm(4, 256, 12), capmoe.make_gemm(4, 256, 64, 257), capmoe.make_gemm(4, (1 << 21) + 8, 64)):
         with pytest.raises(capmoe.CapMoeError):  # the call's own refusals
             capmoe.moe_grouped_gemm_fp8(bad, **{k: v for k, v in a.items() if k != "gemm"}, stream=_NoStream)
+
+
+class _GpuStream(_NoStream):
+    device_index = 0
+
+
+def test_binding_refuses_tensors_of_another_device():
+    x, token, count = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    q, s = capmoe.fp8_row_buffers(4, 64, device="cpu")
+    w = torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+    wq, ws = capmoe.fp8_weight_buffers(2, 8, 64, device="cpu")
+    for call in (lambda: capmoe.moe_quantize_rows(x, token, count, q, s, stream=_GpuStream),
+                 lambda: capmoe.moe_quantize_rows(x, None, None, q, s, stream=_GpuStream),
+                 lambda: capmoe.moe_quantize_weights(w, wq, ws, stream=_GpuStream),
+                 lambda: capmoe.moe_grouped_gemm_fp8(**_product(), stream=_GpuStream),
+                 lambda: capmoe.moe_grouped_gemm_fp8(**_product(src=4), stream=_GpuStream)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+
+
+def test_experts_lie_on_one_device():
+    parts = [t for sizes in ((2, 200, 72), (2, 200, 72), (2, 72, 200)) for t in capmoe.fp8_weight_buffers(*sizes, device="cpu")]
+    for i in range(6):
+        with pytest.raises(ValueError, match="device"):
+            capmoe.Fp8Experts(*parts[:i], parts[i].to("meta"), *parts[i + 1:])
+
+
+def test_ffn_calls_refuse_tensors_of_another_device():
+    desc = _desc(d_model=72, n_experts=2, top_k=1)
+    parts = [t for sizes in ((2, 200, 72), (2, 200, 72), (2, 72, 200)) for t in capmoe.fp8_weight_buffers(*sizes, device="cpu")]
+    experts, x = capmoe.Fp8Experts(*parts), torch.zeros((16, 72), dtype=torch.bfloat16)
+    offset, token, work = torch.zeros(3, dtype=torch.int32), torch.zeros(16, dtype=torch.int32), torch.empty(1 << 20, dtype=torch.uint8)
+    buf = capmoe.LayerBuffers(desc, device="cpu", fp8=True)
+    router = torch.zeros((2, 72))
+    for call in (lambda: capmoe.moe_grouped_ffn_fp8(desc, x, offset, experts, x, work, stream=_GpuStream),
+                 lambda: capmoe.moe_dispatch_ffn_fp8(desc, x, offset, token, experts, x, work, stream=_GpuStream),
+                 lambda: capmoe.moe_layer_forward_fp8(desc, x, router, None, experts, None, 0, buf, stream=_GpuStream)):
+        with pytest.raises(ValueError, match="device"):
+            call()
