@@ -297,6 +297,8 @@ def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
     else:
         _fits(row_token.dtype == _value_dtypes["int32"] and row_token.numel() >= n_rows and row_token.is_contiguous(),
               "row_token: a dense int32 for every row of q")
+    if row_count is not None:
+        _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
     _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
                                     _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows")
 

@@ -311,3 +311,12 @@ def test_ffn_calls_refuse_tensors_of_another_device():
                  lambda: capmoe.moe_layer_forward_fp8(desc, x, router, None, experts, None, 0, buf, stream=_GpuStream)):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+def test_binding_refuses_counts_that_are_no_int32():
+    x = torch.zeros((4, 64), dtype=torch.bfloat16)
+    q, s = capmoe.fp8_row_buffers(4, 64, device="cpu")
+    # an empty tensor has no address: all rows would be done instead of none
+    for bad in (torch.zeros(1), torch.zeros(1, dtype=torch.int64), torch.zeros(0, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="row_count"):
+            capmoe.moe_quantize_rows(x, None, bad, q, s, stream=_NoStream)
