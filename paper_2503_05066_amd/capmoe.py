@@ -358,12 +358,16 @@ class Fp8Experts:
 
     @classmethod
     def quantized(cls, w_gate, w_up, w_down, stream=None):
-        """From w_gate, w_up [E,h,d] and w_down [E,d,h] in bf16 or fp32 (as at model load)."""
+        """From w_gate, w_up [E,h,d] and w_down [E,d,h] in bf16 or fp32 (as at model load).  The tensors belong to `stream`:
+        work on others that uses them waits for it."""
+        import torch
+
         tensors = []
-        for w in (w_gate, w_up, w_down):
-            q, scale = fp8_weight_buffers(*w.shape, device=w.device)
-            moe_quantize_weights(w, q, scale, stream)
-            tensors += [q, scale]
+        with torch.cuda.stream(stream):  # their memory too: what another stream gave back, its work may still write
+            for w in (w_gate, w_up, w_down):
+                q, scale = fp8_weight_buffers(*w.shape, device=w.device)
+                moe_quantize_weights(w, q, scale, stream)
+                tensors += [q, scale]
         return cls(*tensors)
 
 

@@ -512,3 +512,19 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a.y, b.y) and torch.equal(a.expert_offset, b.expert_offset)
+
+
+def test_experts_quantized_on_a_stream_have_memory_of_that_stream(monkeypatch):
+    # memory of another stream may still be written by work on it when the quantising begins
+    side, asked, buffers = torch.cuda.Stream(), [], capmoe.fp8_weight_buffers
+    monkeypatch.setattr(capmoe, "fp8_weight_buffers", lambda *a, **k: (asked.append(torch.cuda.current_stream()), buffers(*a, **k))[1])
+    _, _, weights, _, _ = layer(8, 136, 3, 2, 264)
+    want = capmoe.Fp8Experts.quantized(*weights)
+    assert all(s == torch.cuda.default_stream() for s in asked)
+    torch.cuda.synchronize()
+    asked.clear()
+    got = capmoe.Fp8Experts.quantized(*weights, stream=side)
+    assert len(asked) == 3 and all(s == side for s in asked)
+    assert torch.cuda.current_stream() == torch.cuda.default_stream()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got.tensors, want.tensors))
