@@ -156,7 +156,7 @@ def _stream_on(stream, *tensors):
     if stream is None:
         import torch
 
-        stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream(torch.cuda.current_device())  # 1.3 us; without the argument 2.6
     device = stream.device_index
     for t in tensors:
         if t is not None and t.get_device() != device:
@@ -257,10 +257,10 @@ def _fits(ok, what):
 
 
 @functools.lru_cache(maxsize=None)
-def _dtype(name):
+def _product_dtypes():
     import torch
 
-    return getattr(torch, name)
+    return torch.bfloat16, torch.int32
 
 
 _value_dtypes = {}
@@ -383,43 +383,50 @@ def moe_gemm_query(gemm: MoeGemm) -> int:
 
 
 @functools.lru_cache(maxsize=256)
-def _product_shapes(gemm: bytes):
+def _product_sizes(gemm: bytes):
     """The fields of a MoeGemm that the call accepts, and what they say of the tensors."""
     sizes = MoeGemm.from_buffer_copy(gemm)
     moe_gemm_query(sizes)  # refuses sizes that the call refuses
     pitch, scale_pitch = moe_fp8_query(sizes.n_in)
-    e, blocks = sizes.n_experts, -(-sizes.n_out // 128)
-    return sizes.max_rows, sizes.src_rows, e, sizes.n_out, pitch, scale_pitch, (e, blocks * 128, pitch), (e, blocks, scale_pitch)
+    w = (sizes.n_experts, -(-sizes.n_out // 128) * 128, pitch)
+    w_bytes, w_scale_bytes = math.prod(w), w[0] * (w[1] // 128) * scale_pitch
+    return sizes.max_rows, sizes.src_rows, 4 * (sizes.n_experts + 1), sizes.n_out, pitch, scale_pitch, w, w_bytes, w_scale_bytes
 
 
 def _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
-    """Every tensor against the sizes of the call.  (Of rows that are not gathered, x holds as many as expert_offset ends with,
-    which is known on the device only.)"""
-    max_rows, src_rows, e, n_out, pitch, scale_pitch, w_shape, w_scale_shape = _product_shapes(bytes(gemm))
+    """False if there are no rows, else every tensor against the sizes of the call.  (Of rows that are not gathered, x holds as
+    many as expert_offset ends with, known on the device only.)  In one expression, 1.2 us: one by one the checks took 2 us more, of
+    8 for a token's experts."""
+    max_rows, src_rows, offset_bytes, n_out, pitch, scale_pitch, w_shape, w_bytes, w_scale_bytes = _product_sizes(bytes(gemm))
     if max_rows == 0:
-        return
-    for t in (x, x_scale, expert_offset, w, w_scale, y):
-        if t is None or not t.is_contiguous():
-            raise ValueError("a product of rows takes dense tensors x, x_scale, expert_offset, w, w_scale and y")
-    shape = x.shape
-    rows = shape[0] if shape else 0
-    _fits(shape == (rows, pitch) and x.element_size() == 1, "x: bytes [rows, pitch]")
-    _fits(x_scale.shape == (rows, scale_pitch) and x_scale.element_size() == 1, "x_scale: bytes [rows of x, scale_pitch]")
-    _fits(w.shape == w_shape and w.element_size() == 1, "w: bytes [E, n_out and n_in filled up to multiples of 128]")
-    _fits(w_scale.shape == w_scale_shape and w_scale.element_size() == 1, "w_scale: bytes [E, blocks of n_out, scale_pitch]")
-    shape = y.shape
-    _fits(len(shape) == 2 and shape[1] == n_out and shape[0] >= max_rows and y.dtype == _dtype("bfloat16"), "y: bf16 [max_rows, n_out]")
-    _fits(expert_offset.dtype == _dtype("int32") and expert_offset.numel() > e, "expert_offset: int32 [E + 1]")
-    if row_token is not None:
-        _fits(rows >= src_rows, "x: src_rows rows")
-        _fits(row_token.dtype == _dtype("int32") and row_token.numel() >= max_rows and row_token.is_contiguous(), "row_token: a dense int32 [max_rows]")
+        return False
+    bf16, int32 = _product_dtypes()
+    try:
+        (rows, cols), (y_rows, y_cols) = x.shape, y.shape
+        fits = (cols == pitch and x.nbytes == rows * pitch and x.is_contiguous() and
+                x_scale.nbytes == rows * scale_pitch and x_scale.is_contiguous() and
+                w.shape == w_shape and w.nbytes == w_bytes and w.is_contiguous() and
+                w_scale.nbytes == w_scale_bytes and w_scale.is_contiguous() and
+                y.dtype is bf16 and y_cols == n_out and y_rows >= max_rows and y.is_contiguous() and
+                expert_offset.dtype is int32 and expert_offset.nbytes >= offset_bytes and expert_offset.is_contiguous() and
+                (row_token is None or rows >= src_rows and row_token.dtype is int32 and row_token.nbytes >= 4 * max_rows and
+                 row_token.is_contiguous()))
+    except (AttributeError, ValueError):  # no tensor, or not of two dimensions
+        fits = False
+    if not fits:
+        raise ValueError(f"a product of {max_rows} rows (of {src_rows}, with row_token) takes dense tensors: x bytes [rows, {pitch}], x_scale "
+                         f"bytes [rows, {scale_pitch}], w bytes {list(w_shape)}, w_scale {w_scale_bytes} bytes, y bf16 [max_rows, {n_out}], "
+                         f"expert_offset int32 [{offset_bytes // 4}], row_token int32 [max_rows]")
+    return True
 
 
 def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace, stream=None):
     """workspace may be None where moe_gemm_query answers 0.  A tensor that does not fit the sizes of gemm is refused."""
-    _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y)
-    _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), _ptr(x), _ptr(x_scale), _ptr(row_token), _ptr(expert_offset),
-                                       _ptr(w), _ptr(w_scale), _ptr(y), _ptr(workspace),
+    arrays = (None,) * 7  # without rows none is read
+    if _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
+        arrays = (x.data_ptr(), x_scale.data_ptr(), None if row_token is None else row_token.data_ptr(), expert_offset.data_ptr(),
+                  w.data_ptr(), w_scale.data_ptr(), y.data_ptr())
+    _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), *arrays, _ptr(workspace),
                                        workspace.numel() * workspace.element_size() if workspace is not None else 0,
                                        _stream_on(stream, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace)),
            "moe_grouped_gemm_fp8")
