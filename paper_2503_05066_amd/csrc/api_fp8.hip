@@ -140,10 +140,10 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
     }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-        launch_fp8_thin(up, expert_offset, x, nullptr, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, stream, st);
+        launch_fp8_thin_gate_up(up, expert_offset, x, x_rows, row_token, w, ws.hidden, stream, st);
     }
     ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-    launch_fp8_thin(down, expert_offset, ws.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, stream, st);
+    launch_fp8_thin(down, expert_offset, ws.hidden, nullptr, s.max_rows, nullptr, w.down, w.down_scale, yp, stream, st);
     return hipGetLastError();
 }
 
@@ -238,8 +238,7 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
     const bool streamed = weights_stream((double)g.experts * g.pitch * g.n_pad);
     if (gemm_is_few_rows(g)) {
-        launch_fp8_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr,
-                        nullptr, y, streamed, st);
+        launch_fp8_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, y, streamed, st);
     } else {
         launch_fp8_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);
     }

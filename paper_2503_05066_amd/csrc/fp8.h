@@ -132,9 +132,10 @@ template <int BN, bool SWIGLU>
 void launch_fp8_shape(Fp8Args p, hipStream_t st);
 
 // Kernels for tiles of few rows.  x_scale == nullptr: x is bf16 and is quantised as it is read.
-// up != nullptr: the product of the gate and up weights, and y = silu(gate) * up.
 void launch_fp8_thin(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
-                     const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up, const uint8_t* up_scale,
-                     void* y, bool stream, hipStream_t st);
+                     const int32_t* gather, const void* w, const uint8_t* w_scale, void* y, bool stream, hipStream_t st);
+// .. the products of the gate and the up weights, and y = silu(gate) * up; x is bf16
+void launch_fp8_thin_gate_up(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, int64_t x_rows, const int32_t* gather,
+                             const moe_fp8_experts_t& w, void* y, bool stream, hipStream_t st);
 
 }  // namespace capmoe

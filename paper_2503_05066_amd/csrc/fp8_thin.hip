@@ -350,26 +350,33 @@ static void launch_thin8(Thin8Args a, int64_t tiles, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * a.col_blocks)), dim3(64 * kThin8Waves), lds, st, a);
 }
 
-void launch_fp8_thin(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
-                     const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up, const uint8_t* up_scale,
-                     void* y, bool stream, hipStream_t st) {
+static Thin8Args thin8_args(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
+                            const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up, const uint8_t* up_scale,
+                            void* y) {
     Thin8Args a;
     a.x = x, a.x_scale = x_scale, a.x_rows = x_rows, a.gather = gather, a.expert_offset = expert_offset;
     a.w[0] = (const uint8_t*)w, a.w[1] = (const uint8_t*)up;
     a.w_scale[0] = w_scale, a.w_scale[1] = up_scale;
     a.y = (uint16_t*)y;
     a.experts = g.experts, a.k = g.k, a.pitch = g.pitch, a.n = g.n, a.n_pad = g.n_pad, a.scale_pitch = fp8_scale_pitch(g.k);
-    a.col_blocks = 0;
-    const int64_t tiles = std::min<int64_t>(g.max_rows, g.experts);
-    const int form = (up ? 4 : 0) + (x_scale ? 0 : 2) + (stream ? 1 : 0);
-    switch (form) {
-        case 0: launch_thin8<false, false, false>(a, tiles, st); break;
-        case 1: launch_thin8<false, false, true>(a, tiles, st); break;
-        case 2: launch_thin8<false, true, false>(a, tiles, st); break;
-        case 3: launch_thin8<false, true, true>(a, tiles, st); break;
-        case 6: launch_thin8<true, true, false>(a, tiles, st); break;
-        default: launch_thin8<true, true, true>(a, tiles, st); break;
-    }
+    a.col_blocks = a.split = 0;
+    return a;
+}
+static int64_t thin8_tiles(const Fp8Gemm& g) { return std::min<int64_t>(g.max_rows, g.experts); }
+
+void launch_fp8_thin(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
+                     const int32_t* gather, const void* w, const uint8_t* w_scale, void* y, bool stream, hipStream_t st) {
+    const Thin8Args a = thin8_args(g, expert_offset, x, x_scale, x_rows, gather, w, w_scale, nullptr, nullptr, y);
+    auto launch = x_scale ? (stream ? launch_thin8<false, false, true> : launch_thin8<false, false, false>)
+                          : (stream ? launch_thin8<false, true, true> : launch_thin8<false, true, false>);
+    launch(a, thin8_tiles(g), st);
+}
+
+void launch_fp8_thin_gate_up(const Fp8Gemm& g, const int32_t* expert_offset, const void* x, int64_t x_rows, const int32_t* gather,
+                             const moe_fp8_experts_t& w, void* y, bool stream, hipStream_t st) {
+    const Thin8Args a = thin8_args(g, expert_offset, x, nullptr, x_rows, gather, w.gate, w.gate_scale, w.up, w.up_scale, y);
+    auto launch = stream ? launch_thin8<true, true, true> : launch_thin8<true, true, false>;
+    launch(a, thin8_tiles(g), st);
 }
 
 }  // namespace capmoe
