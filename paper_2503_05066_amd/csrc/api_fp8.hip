@@ -78,39 +78,12 @@ static void launch_fp8_tiles(const Fp8Gemm& g, const int32_t* expert_offset, con
     p.n = g.n, p.n_pad = g.n_pad, p.y_scale_pitch = fp8_scale_pitch(g.n);
     p.col_group = p.tile_shift = 0;
     p.stream = stream;
-    // Narrower tiles where the wide ones would leave compute units without an item: 8 experts of 14336 columns by 4096 (128 wide
-    // items), 8 to 128 rows an expert 110 -> 77, 121 -> 83 us; of 64 x 2048 x 1024 (512) they take 4 % more.
-    const int64_t tiles = g.max_rows / kFfnTileM + std::min<int64_t>(g.max_rows, g.experts);
     if (up)
         launch_fp8_shape<256, true>(p, st);
-    else if (g.n_pad % 256 == 0 && (tiles * (g.n_pad / 256) > 192))
+    else if (fp8_tiles_are_wide(g, compute_units()))
         launch_fp8_shape<256, false>(p, st);
     else
         launch_fp8_shape<128, false>(p, st);
-}
-
-// Weights that the memory-side cache does not keep from one pass to the next are fetched with a policy of their own (see
-// ffn_weights_stream in ffn.hip).
-static bool weights_stream(double bytes) { return bytes > (double)(320ull << 20); }
-
-// Which kernels an FFN or a product takes: those for few rows (fp8_thin.hip) need one launch less, and none for the quantising of
-// x, but make passes of 16 (FFN) or 32 rows over an expert's weights.  Few rows against tiles, FFN: one token, 64 experts of
-// 2048 x 1024 18.9 and 32.1 us, 16 (2 rows an expert) 74.6 and 80.3, 32 (4) 75.8 and 81.5, 48 (6) 86.6 and 81.9, 128 128 and 83;
-// 16 tokens, 8 of 4096 x 14336 (4) 227 and 247, 32 (8) 257 and 240, 64 353 and 247; where the weights are few, and the launches
-// weigh more: 64 tokens, 8 of 2048 x 1024 (16) 24.0 and 31.0; 32 and 64, 1 of 4096 x 2048 26.8 and 38.1, 48.0 and 41.2.
-// Products: 64 of 2048 x 1024, 2 and 4 rows an expert 23.9 and 25.5, 24.2 and 25.6, 16 35.2 and 25.9; 8 of 14336 x 4096, 4 74.1 and 76.9,
-// 16 87.9 and 81.0; 1 of 2056 x 5640, 32, 64, 96 rows 7.9 and 10.6, 10.1 and 11.5, 13.9 and 11.7.
-// The line is drawn on the most rows that the experts may have on average: how they lie is known on the device only (37 tokens, half
-// of them on one of 64 experts of 4096 x 1408: 200 and 187).
-static bool few_weights(double bytes) { return bytes <= (double)(64ull << 20); }
-static bool ffn_is_few_rows(const moe_desc_t& d, const Sizes& s) {
-    const bool few = few_weights(3.0 * d.n_experts * fp8_pitch(d.d_model) * fp8_pitch(d.d_hidden));
-    const int64_t most = std::min<int64_t>((int64_t)s.n_blocks * s.cap, d.n_tokens);  // rows of an expert
-    return s.max_rows <= (few ? 16ll : 4ll) * d.n_experts || most <= (few ? 32 : 16);
-}
-static bool gemm_is_few_rows(const Fp8Gemm& g) {
-    const bool few = few_weights((double)g.experts * g.pitch * g.n_pad);
-    return g.max_rows <= (few ? 32ll : 8ll) * g.experts || g.max_rows <= (few ? 64 : 32);
 }
 
 // The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows.
@@ -119,9 +92,9 @@ static hipError_t launch_ffn_fp8(const moe_desc_t& d, const Sizes& s, const Fp8W
                                  hipStream_t st) {
     const int hp = fp8_pitch(d.d_hidden);
     const Fp8Gemm up = fp8_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp8_gemm(d.n_experts, s.max_rows, hp, d.d_model);
-    const bool stream = weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
+    const bool stream = fp8_weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
     const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
-    if (!ffn_is_few_rows(d, s)) {
+    if (!fp8_ffn_is_few_rows(d, s)) {
         {
             ProfileScope prof(MOE_KERNEL_DISPATCH, st);
             const hipError_t e = launch_quantize_rows(MOE_DTYPE_BF16, x, x_rows, d.d_model, nullptr,
@@ -236,8 +209,8 @@ int moe_grouped_gemm_fp8(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
-    const bool streamed = weights_stream((double)g.experts * g.pitch * g.n_pad);
-    if (gemm_is_few_rows(g)) {
+    const bool streamed = fp8_weights_stream((double)g.experts * g.pitch * g.n_pad);
+    if (fp8_gemm_is_few_rows(g)) {
         launch_fp8_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, y, streamed, st);
     } else {
         launch_fp8_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed, st);

@@ -1,17 +1,9 @@
 // Internal declarations of the 8-bit experts (see include/capmoe.h for the format): e4m3 values, power-of-two scales.
 #pragma once
 
-#include "common.h"
+#include "fp8_forms.h"
 
 namespace capmoe {
-
-constexpr int kFp8Block = 128;          // values of a row, and rows of a weight matrix, that share a scale
-constexpr int kFp8MaxWidth = 1 << 21;   // columns of a matrix: offsets inside a tile of 256 rows stay below 2^32
-constexpr uint32_t kBeyond = 0xfffffff0u;  // a buffer offset that lies behind every window
-
-__host__ __device__ inline int fp8_blocks(int cols) { return (cols + kFp8Block - 1) / kFp8Block; }
-__host__ __device__ inline int fp8_pitch(int cols) { return fp8_blocks(cols) * kFp8Block; }
-__host__ __device__ inline int fp8_scale_pitch(int cols) { return (fp8_blocks(cols) + 3) / 4 * 4; }
 
 // ---------------------------------------------------------------------------------------------
 // quantising on the device
@@ -93,19 +85,6 @@ __device__ __forceinline__ uint32_t max_over_rows_of_16(uint32_t m) {
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-// One product on 8-bit weights as the kernels take it.
-struct Fp8Gemm {
-    int experts;
-    int64_t max_rows;
-    int k;      // columns of the activations as they are
-    int pitch;  // bytes of an 8-bit row: k filled up to a multiple of 128
-    int n;      // output columns
-    int n_pad;  // weight rows of an expert
-};
-inline Fp8Gemm fp8_gemm(int experts, int64_t max_rows, int k, int n) {
-    return Fp8Gemm{experts, max_rows, k, fp8_pitch(k), n, fp8_pitch(n)};
-}
-
 hipError_t launch_quantize_rows(int dtype, const void* x, int64_t n_rows, int cols, const int32_t* row_token,
                                 const int32_t* row_count, void* q, uint8_t* scale, hipStream_t st);
 hipError_t launch_quantize_weights(int dtype, const void* w, int experts, int n_out, int n_in, void* q, uint8_t* scale,

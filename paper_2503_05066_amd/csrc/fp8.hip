@@ -567,7 +567,7 @@ __device__ __forceinline__ int sum_up_to(int v) {
 // The order of the work, found by every wave for itself from the experts' offsets: no launch ahead of this one builds a
 // schedule, whose lists would cost the same two dependent fetches (4 us less for each product or pair of them).
 //
-// First the full row tiles (256 rows, or 128 or 64: see launch_fp8_shape), expert by expert, then what is left of the experts'
+// First the full row tiles (256 rows, or 128 or 64: see fp8_tile_shift), expert by expert, then what is left of the experts'
 // rows, higher tiles first, so that the last items are short ones.  Chunks of `deal` tiles by `group` column blocks go to the
 // XCDs in turn (block id mod 8), and the blocks of an XCD take the items of its chunks in turn.  About as many tiles as an
 // expert has make a chunk: those that run together on an XCD then share weight tiles in its L2, and the XCDs' shares differ little.
@@ -791,14 +791,7 @@ void launch_fp8_shape(Fp8Args p, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
     });
     const int nb = p.n_pad / S::kNCols;
-    const long long active = std::min<long long>(p.max_rows, p.experts);
-    // Lower row tiles as long as their items still fit one round of the chip's 256 compute units (the bound counts a partly
-    // filled tile of every expert).  Tiles of 64, 128, 256 rows, us: one expert, 203 rows of 2056 x 5640 11.8, 14.4, 17.6, 512 rows
-    // 20.0, 15.7, 19.5, 1024 29.5, 26.9, 23.6; the FFN of one expert of 4096 x 2048, 512 tokens 45.5, 54.9, 77.1, 2048 95.6, 82.3, 96.0 (its
-    // products take different ones: 73.5), 4096 162, 131, 112; 512 tokens top-2 on 8 experts of 2048 x 1024 34.1, 39.4, 38.5, 1024 45.9, 42.8,
-    // 55.7, 2048 62.2, 56.1, 60.4 (taken: 35.5, 46.6, 60.2); 1500 on 8 of 4096 x 4096 247, 202, 168.
-    p.tile_shift = 8;
-    while (p.tile_shift > 6 && nb * ((p.max_rows >> (p.tile_shift - 1)) + active) <= 256 + 32) --p.tile_shift;
+    p.tile_shift = fp8_tile_shift(p.max_rows, p.experts, nb, compute_units());
     // a block per compute unit, the same number on every XCD (which of them get items is known on the device only)
     const int grid = 8 * std::max(1, compute_units() / 8);
     p.col_group = nb % 4 == 0 ? 4 : (nb % 3 == 0 ? 3 : (nb % 2 == 0 ? 2 : 1));

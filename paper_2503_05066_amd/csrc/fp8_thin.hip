@@ -2,7 +2,7 @@
 // small capacity.
 //
 // The work is streaming weights.  A wave has 32 weight rows: 32 output columns, or the gate and up rows of 16 hidden
-// columns.  The four waves of a block take different rows or parts of K (see thin_split) and share nothing until the end: each
+// columns.  The four waves of a block take different rows or parts of K (see fp8_thin_split) and share nothing until the end: each
 // keeps a ring of its own in LDS, filled by direct loads, waits for its own slabs only and needs no barrier (as the bf16 kernel,
 // ffn_thin.hip).  Two blocks share a compute unit.
 //
@@ -326,15 +326,6 @@ __global__ __launch_bounds__(64 * kThin8Waves, 2) void fp8_thin_kernel(const Thi
     }
 }
 
-// How many waves share a weight row.  2048 waves fill the chip; whole rows keep a wave's ring full for longer, shorter parts
-// end sooner.  Products at 4, 2, 1: one token's 8 experts of 64 x 2048 x 1024 (512 waves with whole rows) FFN 18.6, 19.4, 24.9 us;
-// two tokens' (960) 32.7, 27.0, 27.2; four tokens' (2048) 58, 48, 41; 16 tokens', 108, 86, 75; 64 x 4096 x 1408 (5632) 227, 190, 185;
-// 8 experts of 14336 columns by 4096 (1024, but long) 73.4, 77.0, 76.4.
-static int thin_split(int64_t waves, int slabs) {
-    if (waves <= 512 || (waves <= 1024 && slabs >= 64)) return 4;
-    return waves <= 1024 ? 2 : 1;
-}
-
 template <bool SWIGLU, bool QUANT, bool STREAM>
 static void launch_thin8(Thin8Args a, int64_t tiles, hipStream_t st) {
     constexpr int lds = kThin8Waves * kThin8RingBytes;
@@ -344,7 +335,7 @@ static void launch_thin8(Thin8Args a, int64_t tiles, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     });
     constexpr int cols = Thin8<16, SWIGLU, QUANT, STREAM>::kCols;
-    a.split = thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kFp8Block);
+    a.split = fp8_thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kFp8Block, compute_units());
     const int per_block = kThin8Waves / a.split * cols;
     a.col_blocks = (a.n + per_block - 1) / per_block;
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * a.col_blocks)), dim3(64 * kThin8Waves), lds, st, a);
