@@ -40,17 +40,24 @@ inline bool fp8_weights_stream(double bytes) { return bytes > (double)(320ull <<
 // weigh more: 64 tokens, 8 of 2048 x 1024 (16) 24.0 and 31.0; 32 and 64, 1 of 4096 x 2048 26.8 and 38.1, 48.0 and 41.2.
 // Products: 64 of 2048 x 1024, 2 and 4 rows an expert 23.9 and 25.5, 24.2 and 25.6, 16 35.2 and 25.9; 8 of 14336 x 4096, 4 74.1 and 76.9,
 // 16 87.9 and 81.0; 1 of 2056 x 5640, 32, 64, 96 rows 7.9 and 10.6, 10.1 and 11.5, 13.9 and 11.7.
-// The line is drawn on the most rows that the experts may have on average: how they lie is known on the device only (37 tokens, half
-// of them on one of 64 experts of 4096 x 1408: 200 and 187).
+// How the rows lie is known on the device only, and the passes over a long expert run one after the other in its own blocks, so the most
+// rows that an expert may have are four passes.  Few rows against tiles, dealt evenly, half on one expert, all on one (FFN: on as few as hold
+// them): products, 64 of 2048 x 1024, 128 rows 25.9 and 28.3, 43.3 and 39.3, 36.8 and 14.6, 512 26.3 and 29.2, 93.5 and 39.6, 140 and 15.6;
+// 60 of 512 x 1280, 120 rows 13.3 and 16.9, 13.4 and 16.7, 14.8 and 12.0, 960 13.7 and 17.1, 54 and 21, 93 and 17; 256 of 512 x 512, 8192 rows
+// 19.6 and 22.3, 395 and 34, 769 and 19.5; 8 of 14336 x 4096, 64 rows 72.5 and 74.2, 80 and 80, 32 and 63.  FFN: 16 of 1024 x 1024, 64 tokens
+// top-4 18.6 and 28.8, 37.4 and 31.0, 31.7 and 25.4; 128 of 2048 x 768, 64 top-8 111 and 113, 161 and 112, 72 and 36; 256 of 256 x 256, 128 top-8
+// 21 and 34, 57 and 41, 43 and 25, 512 top-8 22 and 35, 171 and 52, 158 and 32.  (Over plans whose experts' shares are e^x of normal x, Zipf's or
+// one in twenty's, products of 64 to 127 rows take 0.87 of the tiles' time, of 1024 and more 1.31, at worst 4.6.)
+constexpr int kFp8MostPasses = 4;
 inline bool fp8_few_weights(double bytes) { return bytes <= (double)(64ull << 20); }
 inline bool fp8_ffn_is_few_rows(const moe_desc_t& d, const Sizes& s) {
     const bool few = fp8_few_weights(3.0 * d.n_experts * fp8_pitch(d.d_model) * fp8_pitch(d.d_hidden));
     const int64_t most = std::min<int64_t>((int64_t)s.n_blocks * s.cap, d.n_tokens);  // rows of an expert
-    return s.max_rows <= (few ? 16ll : 4ll) * d.n_experts || most <= (few ? 32 : 16);
+    return most <= (few ? 32 : 16) || (most <= kFp8MostPasses * 16 && s.max_rows <= (few ? 16ll : 4ll) * d.n_experts);
 }
 inline bool fp8_gemm_is_few_rows(const Fp8Gemm& g) {
     const bool few = fp8_few_weights((double)g.experts * g.pitch * g.n_pad);
-    return g.max_rows <= (few ? 32ll : 8ll) * g.experts || g.max_rows <= (few ? 64 : 32);
+    return g.max_rows <= (few ? 64 : 32) || (g.max_rows <= kFp8MostPasses * 32 && g.max_rows <= (few ? 32ll : 8ll) * g.experts);
 }
 
 // Which width a product on high tiles takes, 256 or 128 columns: narrower tiles where the wide ones would leave a quarter of the

@@ -54,7 +54,7 @@ int main() {
 NONE = capmoe.MODE_NONE
 PRODUCTS = [  # rows, experts, columns of x, columns of y -> on 256, 128 and 32 compute units
     ((8, 64, 2048, 1024), ("few/4", "few/4", "few/1")),
-    ((512, 64, 2048, 1024), ("few/1", "few/1", "few/1")),
+    ((128, 64, 2048, 1024), ("few/1", "few/1", "few/1")),
     ((203, 1, 2056, 5640), ("128x64", "128x128", "128x256")),  # 45 column blocks: 180 items of 64 rows, 90 of 128
     ((1024, 1, 2056, 5640), ("128x256",) * 3),
     ((1024, 8, 4096, 14336), ("256x256 stream",) * 3),
@@ -96,3 +96,22 @@ def test_forms_of_a_product_follow_the_compute_units(ask, sizes, forms):
 @pytest.mark.parametrize("sizes,forms", FFNS, ids=lambda v: "-".join(map(str, v)) if isinstance(v[0], int) else "")
 def test_forms_of_an_ffn_follow_the_compute_units(ask, sizes, forms):
     assert tuple(ask("f", cus, sizes) for cus in UNITS) == forms
+
+
+# An expert may have all rows of a product, and a row of every token in an FFN: at most four passes over its weights, 32 and 16 rows each.
+@pytest.mark.parametrize("e,k,n", [(256, 512, 512), (64, 2048, 1024), (60, 512, 1280), (128, 2048, 768)])
+def test_products_whose_rows_may_lie_on_one_expert(ask, e, k, n):
+    assert ask("p", 256, (128, e, k, n)).startswith("few")
+    for rows in (129, 512, 8 * e, 32 * e):
+        assert ask("p", 256, (rows, e, k, n))[:3] in ("128", "256")
+
+
+@pytest.mark.parametrize("e,top_k,d,h", [(256, 8, 256, 256), (128, 4, 2048, 768), (64, 4, 2048, 1024), (64, 8, 512, 512)])
+def test_ffns_whose_tokens_may_lie_on_the_same_experts(ask, e, top_k, d, h):
+    assert ask("f", 256, (64, e, top_k, d, h)).startswith("few")
+    for tokens in (65, 128, 512):
+        assert ask("f", 256, (tokens, e, top_k, d, h))[:3] in ("128", "256")
+    # a capacity bounds them too: one pass, and four
+    tokens = 16 * e // top_k
+    assert ask("f", 256, (tokens, e, top_k, d, h), capmoe.MODE_TOKEN_DROP, 1.0).startswith("few")
+    assert ask("f", 256, (tokens, e, top_k, d, h), capmoe.MODE_TOKEN_DROP, 4.0).startswith("few") == (3 * e * d * h <= 64 << 20)
