@@ -115,3 +115,12 @@ def test_ffns_whose_tokens_may_lie_on_the_same_experts(ask, e, top_k, d, h):
     tokens = 16 * e // top_k
     assert ask("f", 256, (tokens, e, top_k, d, h), capmoe.MODE_TOKEN_DROP, 1.0).startswith("few")
     assert ask("f", 256, (tokens, e, top_k, d, h), capmoe.MODE_TOKEN_DROP, 4.0).startswith("few") == (3 * e * d * h <= 64 << 20)
+
+
+def test_gpu_cases_have_the_forms_that_they_name(ask):
+    import test_gpu_fp8 as on_gpu
+
+    for counts, k, n, form in on_gpu.PRODUCT_FORMS + on_gpu.STREAMED_PRODUCTS:
+        assert ask("p", 256, (sum(counts), len(counts), k, n)) == form, (counts, k, n)
+    for tokens, k, counts, d, h, forms in on_gpu.STREAMED_FFNS:
+        assert ask("f", 256, (tokens, len(counts), k, d, h)) == forms, (tokens, d, h)

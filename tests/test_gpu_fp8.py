@@ -528,3 +528,120 @@ def test_experts_quantized_on_a_stream_have_memory_of_that_stream(monkeypatch):
     assert torch.cuda.current_stream() == torch.cuda.default_stream()
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got.tensors, want.tensors))
+
+
+# Cases by the form that the call takes (test_fp8_forms.py holds the forms against the rules): few rows with 4, 2 or 1 waves to a weight
+# row, or column width x row tile.  (rows per expert, columns of x, columns of y, form)
+PRODUCT_FORMS = [
+    ([128], 520, 264, "128x64"), ([0, 60, 0, 4], 1416, 264, "few/4"), ([0, 120, 0, 8], 264, 392, "few/4"),
+    ([1, 0] * 8 + [70, 0, 22], 136, 1032, "few/2"), ([3, 0, 1, 40] + [1] * 16 + [33], 640, 1000, "few/2"),
+    ([0, 1] * 20 + [65, 0, 33], 520, 1032, "few/1"), ([100] + [0, 1] * 14, 1032, 2056, "few/1"),
+    ([40, 1, 0, 20, 33, 0, 9, 3, 2, 1, 12, 8], 392, 4352, "256x64"), ([100, 1, 0, 130, 33, 200, 9, 3, 64, 128, 12, 88], 520, 4096, "256x128"),
+    ([128, 1, 0, 256, 33, 127, 9, 3, 64, 128, 12, 7], 1152, 4096, "256x128"), ([300, 1, 0, 20], 1032, 136, "128x64"), ([700, 1, 400], 264, 2048, "128x128")]
+
+
+@pytest.mark.parametrize("counts,k,n,form", PRODUCT_FORMS)
+def test_product_of_every_form(counts, k, n, form):
+    p = Product(counts, k, n)
+    p.check(p.run())
+    p = Product(counts, k, n, src=31)
+    p.check(p.run())
+
+
+# offsets from elsewhere, within P_max: capacities of 16 rows, 128 in all, and an expert with up to all of them
+@pytest.mark.parametrize("counts", [[0, 0, 128, 0, 0, 0, 0, 0], [16, 17, 33, 0, 0, 1, 0, 50], [1, 0, 0, 100, 2, 17, 0, 1], [64, 0, 0, 0, 0, 0, 0, 64]])
+def test_ffn_of_few_rows_with_long_experts(counts):
+    desc, x, weights, _, _ = layer(128, 264, 8, 1, 392, mode=capmoe.MODE_TOKEN_DROP, capacity_scope=capmoe.SCOPE_GLOBAL, gamma=1.0)
+    assert capmoe.moe_query(desc)[0] == 16 and capmoe.moe_query(desc)[2] == 128
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    rows, token = int(offset[-1]), rng(12).integers(0, 128, 128).astype(np.int32)
+    experts = capmoe.Fp8Experts.quantized(*weights)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    yp = torch.full((128, 264), 7.0, dtype=BF16, device="cuda")
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(token), experts, yp, ws)
+    assert torch.all(yp[rows:] == 7.0)
+    values = [ref.weights_value(*ref.quantize_weights(plain(w))) for w in weights]
+    want = ref.ffn(plain(x), *values, offset, token[:rows])[:, :264]
+    off = plain(yp[:rows]) - want
+    assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want)
+    assert np.abs(off).max() <= 0.5 * np.maximum(np.sqrt(np.mean(want ** 2)), np.abs(want).max() / 8)
+
+
+def device_value(q, s):
+    """8-bit weights [n, k] of an expert with their scales, in 64 bits on the device."""
+    return q.view(torch.float8_e4m3fn).double() * torch.exp2(s[:, : q.shape[1] // 128].double() - 127).repeat_interleave(128, 0).repeat_interleave(128, 1)
+
+
+def streamed_weights(e, n, k, seed):
+    """More 8-bit weights than the memory-side cache holds, normal values of sizes that differ from block to block."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, s = capmoe.fp8_weight_buffers(e, n, k)
+    for i in range(e):
+        w = torch.randn((n // 128, 128, k // 128, 128), generator=g, device="cuda") * k ** -0.5
+        w *= torch.exp2(torch.randint(-2, 3, (n // 128, 1, k // 128, 1), generator=g, device="cuda").float())
+        capmoe.moe_quantize_weights(w.view(1, n, k), q[i:i + 1], s[i:i + 1])
+    return q, s
+
+
+# every height in steps of 32 rows, and experts with two tiles (whose weights are kept)
+HEIGHTS = [256, 225, 200, 161, 129, 100, 65, 40, 31, 300, 0, 1]
+STREAMED_PRODUCTS = [(HEIGHTS, 8320, 4096, "256x256 stream"), (HEIGHTS, 7168, 4096, "256x256 stream"), (HEIGHTS, 8192, 3712, "128x256 stream"),
+                     ([5, 0, 1, 16, 9, 0, 2, 30, 0, 1, 0, 0], 8320, 4096, "few/1 stream"), ([1, 0, 1, 0, 0, 2, 0, 0, 1, 0, 0, 0], 8320, 4096, "few/4 stream"),
+                     ([1, 0, 1, 0, 0, 2, 0, 0, 1, 0, 0, 0], 7168, 4096, "few/2 stream")]
+
+
+@pytest.mark.parametrize("counts,k,n,form", STREAMED_PRODUCTS)
+def test_streamed_product_of_every_form(counts, k, n, form):
+    # odd and even numbers of slabs: walks over k that begin in the middle wrap around at either half of a word of scales
+    q, s = streamed_weights(len(counts), n, k, 1)
+    rows = sum(counts)
+    x = rng(21, rows, k).standard_normal((rows, k)) * np.exp2(rng(22).integers(-2, 3, (rows, k // 128))).repeat(128, 1)
+    xq, xs = capmoe.fp8_row_buffers(rows, k)
+    capmoe.moe_quantize_rows(on(x, BF16), None, None, xq, xs)
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    y = torch.full((rows, n), 7.0, dtype=BF16, device="cuda")
+    capmoe.moe_grouped_gemm_fp8(capmoe.make_gemm(rows, k, n, len(counts)), xq, xs, None, on(offset), q, s, y, None)
+    xv = on(ref.rows_value(xq.cpu().numpy(), xs.cpu().numpy()))
+    for i in range(len(counts)):
+        a, w = xv[offset[i]:offset[i + 1]], device_value(q[i], s[i])
+        want, mag = a @ w.T, a.abs() @ w.abs().T
+        off = (y[offset[i]:offset[i + 1]].double() - want).abs()
+        assert bool((off <= 2.0 ** -8 * want.abs() + 2.0 ** -12 * mag).all()), i
+
+
+# tokens, top-k, rows per expert, d, h, forms of the two products
+STREAMED_FFNS = [(600, 4, HEIGHTS, 4096, 2304, "128x256 256x256 stream"), (600, 4, HEIGHTS, 4224, 2432, "128x256 128x256 stream"),
+                 (600, 4, HEIGHTS, 4352, 2304, "128x256 256x256 stream"),
+                 (16, 2, [16, 3, 0, 1, 9, 0, 2, 0, 0, 1, 0, 0], 4224, 2432, "few/1 few/1 stream"), (2, 2, [0, 2, 0, 0, 0, 1, 0, 0, 0, 0, 1, 0], 4096, 2304, "few/2 few/4 stream"),
+                 (1, 2, [0, 0, 0, 1, 0, 0, 0, 0, 0, 0, 0, 1], 4224, 2432, "few/4 few/4 stream")]
+
+
+@pytest.mark.parametrize("tokens,k,counts,d,h,forms", STREAMED_FFNS)
+def test_streamed_ffn_of_every_form(tokens, k, counts, d, h, forms):
+    e, rows = len(counts), sum(counts)
+    desc = capmoe.make_desc(tokens, d, e, k, h, mode=capmoe.MODE_NONE)
+    parts = [streamed_weights(e, n, c, seed) for seed, (n, c) in enumerate(((h, d), (h, d), (d, h)))]
+    experts = capmoe.Fp8Experts(*[t for p in parts for t in p])
+    x = on(rng(31, tokens).standard_normal((tokens, d)), BF16)
+    offset, token = plan_of(rng(32, tokens), tokens, counts)
+    padded = np.zeros(tokens * k, np.int32)
+    padded[:rows] = token
+    yp = torch.full((tokens * k, d), 7.0, dtype=BF16, device="cuda")
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xA5)
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(padded), experts, yp, ws)
+    assert torch.all(yp[rows:] == 7.0)
+    xv = on(ref.rows_value(*ref.quantize_rows(plain(x)))[token])
+    want = np.zeros((rows, d))
+    for i in np.flatnonzero(counts):
+        gate, up, down = (device_value(q[i], s[i]) for q, s in parts)
+        a = xv[offset[i]:offset[i + 1]]
+        g, u = plain(a @ gate.T), plain(a @ up.T)
+        hidden = ref.rows_value(*ref.quantize_rows(ref.to_bf16(g / (1 + np.exp(-g)) * u)))
+        want[offset[i]:offset[i + 1]] = plain(on(hidden) @ down.T)
+    off = plain(yp[:rows]) - want
+    assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want), np.linalg.norm(off) / np.linalg.norm(want)
+    # a row's own error: eight of its 2304 or more hidden values, or one of ten times their mean square, on the other side of a border
+    # are 2^-3 * 10 / 48 = 2^-5.3, and the two roundings
+    err = np.linalg.norm(off, axis=1) / np.linalg.norm(want, axis=1)
+    assert np.all(err <= 2.0 ** -5), (np.argmax(err), err.max())
