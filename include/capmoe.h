@@ -245,9 +245,9 @@ int moe_layer_forward(const moe_desc_t* desc, const void* x, const float* w_rout
  *
  * The 8-bit form of a matrix of c columns has rows of pitch = 128 * ceil(c / 128) bytes, one e4m3 value each, zero behind
  * column c, and one scale byte per row and 128 columns in rows of scale_pitch = 4 * ceil(c / 512) bytes, zero behind the
- * last: the value is e4m3 * 2^(byte - 127).  Expert weights [E,n,c] have n filled up to a multiple of 128 with rows of zeros
- * and one scale byte per 128 rows x 128 columns: values [E, 128 * ceil(n / 128), pitch], scales [E, ceil(n / 128),
- * scale_pitch].  Values are 16-byte aligned, scales 4-byte aligned.
+ * last: the value is e4m3 * 2^(byte - 127), with byte 255 not a number (quantising gives at most 247).  Expert weights [E,n,c]
+ * have n filled up to a multiple of 128 with rows of zeros and one scale byte per 128 rows x 128 columns: values
+ * [E, 128 * ceil(n / 128), pitch], scales [E, ceil(n / 128), scale_pitch].  Values are 16-byte aligned, scales 4-byte aligned.
  *   Quantising: the byte of a block is the smallest b >= 0 with amax <= 448 * 2^(b - 127), amax over the block's finite
  *   values; every value is divided by 2^(b - 127) (exactly) and rounded once to e4m3, to nearest even; NaN and infinities
  *   become NaN (0x7F).  So a value is off by at most 2^-4 of itself, or by 2^-10 * 2^(b - 127) where that is more.

@@ -645,3 +645,24 @@ def test_streamed_ffn_of_every_form(tokens, k, counts, d, h, forms):
     # are 2^-3 * 10 / 48 = 2^-5.3, and the two roundings
     err = np.linalg.norm(off, axis=1) / np.linalg.norm(want, axis=1)
     assert np.all(err <= 2.0 ** -5), (np.argmax(err), err.max())
+
+
+@pytest.mark.parametrize("counts", [[5, 12], [300, 12]])
+def test_a_scale_byte_of_255_is_not_a_number(counts):
+    # and those behind the last block stand for nothing
+    p = Product(counts, 520, 264)
+    p.xs[:, 5:], p.ws[:, :, 5:] = 255, 255
+    p.check(p.run())
+    p.xs[3, 1], p.ws[1, 1, 4] = 255, 255
+    got = plain(p.run())
+    nan = np.zeros(got.shape, bool)
+    nan[3], nan[counts[0]:, 128:256] = True, True
+    assert np.array_equal(np.isnan(got), nan)
+
+
+@pytest.mark.parametrize("counts", [[5, 12], [300, 12]])
+def test_the_largest_and_smallest_scale_bytes(counts):
+    # 2^127 and 2^-127 meet as 1
+    p = Product(counts, 520, 264)
+    p.xs[:, :5], p.ws[:, :, :5] = [254, 0, 254, 0, 254], [0, 254, 0, 254, 0]
+    p.check(p.run())
