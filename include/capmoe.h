@@ -312,8 +312,9 @@ int moe_query_fp8(const moe_desc_t* desc, size_t* workspace_bytes);
 
 /*
  * moe_grouped_ffn, moe_dispatch_ffn and moe_layer_forward with 8-bit experts.  desc->dtype is MOE_DTYPE_BF16 (the type of
- * xp / x, yp and y); any other is MOE_ERR_UNSUPPORTED.  d is a multiple of 8, h any number; d and h at most 2^21.  The
- * activations are quantised on the way: xp / x by rows, and the hidden activation, rounded to bf16 once, by rows too.
+ * xp / x, yp and y); any other is MOE_ERR_UNSUPPORTED.  d is a multiple of 8, h any number (moe_quantize_weights takes the down
+ * weights of an h that is no multiple of 8 with columns of zeros up to the next, which have the same 8-bit form); d and h at most
+ * 2^21.  The activations are quantised on the way: xp / x by rows, and the hidden activation, rounded to bf16 once, by rows too.
  * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp8 and moe_layer_forward_fp8: N * d < 2^31 and
  * N * pitch(d) < 2^32 - 15; all three: P_max * ceil(max(d, h) / 128) < 2^31; else MOE_ERR_UNSUPPORTED.  Where no row can
  * survive (P_max = 0) nothing is enqueued for the FFN, and x, xp, row_token and yp may be null.

@@ -666,3 +666,22 @@ def test_the_largest_and_smallest_scale_bytes(counts):
     p = Product(counts, 520, 264)
     p.xs[:, :5], p.ws[:, :, :5] = [254, 0, 254, 0, 254], [0, 254, 0, 254, 0]
     p.check(p.run())
+
+
+@pytest.mark.parametrize("tokens,counts", [(12, [12, 3, 0, 9]), (300, [300, 64, 0, 211])])
+def test_hidden_widths_that_are_no_multiple_of_8(tokens, counts):
+    # the down weights of such a width are quantised with columns of zeros behind it
+    desc, x, (gate, up, down), _, _ = layer(tokens, 264, 4, 3, 203, mode=capmoe.MODE_NONE)
+    with pytest.raises(capmoe.CapMoeError):
+        capmoe.Fp8Experts.quantized(gate, up, down)
+    experts = capmoe.Fp8Experts.quantized(gate, up, torch.nn.functional.pad(down, (0, 5)))
+    offset, token = plan_of(rng(5, tokens), tokens, counts)
+    ws = torch.empty(capmoe.moe_query_fp8(desc), dtype=torch.uint8, device="cuda")
+    yp = torch.zeros((capmoe.moe_query(desc)[2], 264), dtype=BF16, device="cuda")
+    padded = np.zeros(yp.shape[0], np.int32)
+    padded[:len(token)] = token
+    capmoe.moe_dispatch_ffn_fp8(desc, x, on(offset), on(padded), experts, yp, ws)
+    values = [ref.weights_value(*ref.quantize_weights(plain(w))) for w in (gate, up, down)]
+    want = ref.ffn(plain(x), *values, offset, token)[:, :264]
+    off = plain(yp)[:len(token)] - want
+    assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want)
