@@ -90,8 +90,8 @@ struct Fills8 {
         sa = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x_scale + x0 * p.scale_pitch), 0,
                                                (int)(uint32_t)min((p.x_rows - x0) * p.scale_pitch, (int64_t)kBeyond), kRsrcFlags);
         const size_t n_at = (size_t)w.e * p.n_pad + w.n0;
-        b0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[0] + n_at * p.pitch), 0, S::kNCols * p.pitch, kRsrcFlags);
-        b1 = S::SWIGLU ? __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[1] + n_at * p.pitch), 0, S::kNCols * p.pitch, kRsrcFlags) : b0;
+        b0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[0] + n_at * p.pitch), 0, -1, kRsrcFlags);
+        b1 = S::SWIGLU ? __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[1] + n_at * p.pitch), 0, -1, kRsrcFlags) : b0;
         // a wave's weight rows lie in one block of 128 (with SWIGLU in one of either tensor)
         scale_at = (n_at / kFp8Block + (S::SWIGLU || S::BN == 128 ? 0 : wn)) * p.scale_pitch;
         sb0 = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w_scale[0] + scale_at), 0, p.scale_pitch, kRsrcFlags);
