@@ -152,14 +152,14 @@ def _stream(stream):
 
 def _stream_on(stream, *tensors):
     """_stream for calls that look at their tensors: all of them lie on the stream's device (host memory, or another GPU's, is
-    no address of a kernel there)."""
+    no address of a kernel there).  A handle that names no device is not compared."""
     if stream is None:
         import torch
 
         stream = torch.cuda.current_stream(torch.cuda.current_device())  # 1.3 us; without the argument 2.6
-    device = stream.device_index
+    device = getattr(stream, "device_index", None)
     for t in tensors:
-        if t is not None and t.get_device() != device:
+        if t is not None and t.get_device() != device and device is not None:
             raise ValueError(f"a tensor on {t.device}, a stream of device {device}")
     return stream.cuda_stream
 
@@ -428,8 +428,7 @@ def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale,
                   w.data_ptr(), w_scale.data_ptr(), y.data_ptr())
     _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), *arrays, _ptr(workspace),
                                        workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                       _stream_on(stream, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace)),
-           "moe_grouped_gemm_fp8")
+                                       _stream_on(stream, x, x_scale, row_token, expert_offset, w, w_scale, y)), "moe_grouped_gemm_fp8")
 
 
 def moe_query_fp8(desc: MoeDesc) -> int:

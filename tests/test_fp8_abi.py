@@ -320,3 +320,15 @@ def test_binding_refuses_counts_that_are_no_int32():
     for bad in (torch.zeros(1), torch.zeros(1, dtype=torch.int64), torch.zeros(0, dtype=torch.int32)):
         with pytest.raises(ValueError, match="row_count"):
             capmoe.moe_quantize_rows(x, None, bad, q, s, stream=_NoStream)
+
+
+def test_calls_that_ran_without_a_device_to_compare_still_run():
+    class Handle:  # of a stream that something else made
+        cuda_stream = None
+
+    a = _product(rows=0)
+    capmoe.moe_grouped_gemm_fp8(**a, stream=Handle)
+    # a workspace of no bytes, wherever it is
+    a["workspace"] = torch.empty(0, dtype=torch.uint8, device="meta")
+    b = {k: v for k, v in a.items() if k in ("gemm", "row_token", "workspace")}
+    capmoe.moe_grouped_gemm_fp8(**b, x=None, x_scale=None, expert_offset=None, w=None, w_scale=None, y=None, stream=_GpuStream)
