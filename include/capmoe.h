@@ -334,6 +334,107 @@ int moe_layer_forward_fp8(const moe_desc_t* desc, const void* x, const float* w_
                           int32_t* pair_row, void* yp, void* y, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Experts in 4 bits (OCP microscaled e2m1: a power-of-two scale for each 32 values of a row, which the matrix instructions of
+ * gfx950 apply themselves).
+ *
+ * The 4-bit form of a matrix of c columns has rows of pitch = 128 * ceil(c / 256) bytes, two e2m1 codes each, the lower column in
+ * the lower four bits, zero behind column c, and rows of scale_pitch = 16 * ceil(c / 512) scale bytes, zero behind the last.  The
+ * byte of the b-th 32 columns of a group of 512 has place 4 * (b % 4) + b / 4 of the group's 16 (a lane of the matrix
+ * instructions reads four places as one word); a value is e2m1 * 2^(byte - 127), and byte 255 makes its 32 values no numbers.
+ * Expert weights [E,n,c] have n filled up to a multiple of 128 with rows of zeros: values [E, 128 * ceil(n / 128), pitch], scales
+ * [E, 128 * ceil(n / 128), scale_pitch].  Values and scales are 16-byte aligned.
+ *   Quantising: the byte of a block is the smallest b >= 0 with amax <= 6 * 2^(b - 127), so nothing saturates; every value is
+ *   divided by 2^(b - 127) (exactly) and rounded once to 0, 0.5, 1, 1.5, 2, 3, 4 or 6, ties to the even code.  A block that holds a NaN
+ *   or an infinity gets byte 255 and codes of zero.
+ */
+
+/* pitch and scale_pitch of a 4-bit matrix of `cols` columns, in bytes (host only; either may be NULL). */
+int moe_fp4_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch);
+
+/*
+ * Rows of activations to 4 bits, on the way permuted if row_token is given: as moe_quantize_rows, with this format.  cols a
+ * multiple of 8 (bf16) or 4 (fp32), at most 2^21; n_rows < 2^31 and n_rows * ceil(cols / 512) < 2^31, else MOE_ERR_UNSUPPORTED.
+ */
+int moe_quantize_rows_fp4(int dtype, const void* x, int64_t n_rows, int32_t cols, const int32_t* row_token,
+                          const int32_t* row_count, void* q, uint8_t* scale, void* stream);
+
+/* Expert weights w [n_experts, n_out, n_in] in dtype to 4 bits, padding included; n_in and the rows, filled up, of all experts as
+ * cols and n_rows above, n_out at most 2^21. */
+int moe_quantize_weights_fp4(int dtype, const void* w, int32_t n_experts, int32_t n_out, int32_t n_in, void* q,
+                             uint8_t* scale, void* stream);
+
+/*
+ * The values that 4-bit (bits = 4) or 8-bit rows (bits = 8: of moe_quantize_rows, not of weights) stand for: y [n_rows,cols] in dtype, rounded
+ * once (bf16 holds all of them down to 2^-133, fp32 all).  4-bit weights are rows of E * 128 * ceil(n / 128).  Sizes as above.
+ */
+int moe_dequantize_rows(int bits, int dtype, const void* q, const uint8_t* scale, int64_t n_rows, int32_t cols, void* y,
+                        void* stream);
+
+/* A norm of rows (host memory, plain data). */
+typedef struct {
+    int32_t n_rows;
+    int32_t cols;   /* a multiple of 8 (bf16) or 4 (fp32), at most 2^21                                        */
+    int32_t dtype;  /* MOE_DTYPE_* of x, residual, weight, sum and y                                           */
+    int32_t bits;   /* 0; 8 or 4: q and scale get the rows in that form (moe_fp8_query, moe_fp4_query)         */
+    float eps;      /* added to the mean square: a normal fp32 number above 0                                  */
+} moe_norm_t;
+
+/*
+ * The residual's addition and the root-mean-square norm ahead of a layer:
+ *   h = x + residual, rounded to dtype (h = x without one)      sum = h
+ *   y = h / sqrt(mean over the columns of h^2 + eps) * weight   computed in fp32, rounded to dtype once
+ *   q, scale = the 8- or 4-bit form of y as rounded             the bytes of moe_quantize_rows (_fp4) on y
+ * residual, weight [cols], row_count (device: rows behind *row_count stay untouched), sum, and with bits also y may be NULL; with
+ * bits = 0 q and scale are ignored.  sum and y may be x or residual themselves, but not the same array; no other arrays may overlap.
+ * n_rows * ceil(cols / 512) < 2^31, else MOE_ERR_UNSUPPORTED.  Rows whose squares pass the range of fp32 are normed all the same.
+ */
+int moe_norm_rows(const moe_norm_t* norm, const void* x, const void* residual, const void* weight, const int32_t* row_count,
+                  void* sum, void* y, void* q, uint8_t* scale, void* stream);
+
+/*
+ * Matrix product grouped by expert of 4-bit rows and 4-bit weights: as moe_grouped_gemm_fp8, with these formats and without a
+ * workspace.
+ */
+int moe_grouped_gemm_fp4(const moe_gemm_t* gemm, const void* x, const uint8_t* x_scale, const int32_t* row_token,
+                         const int32_t* expert_offset, const void* w, const uint8_t* w_scale, void* y, void* stream);
+
+/* The 4-bit weights of a layer's experts: gate and up [E,h,d], down [E,d,h] (device pointers, host struct). */
+typedef struct {
+    const void* gate;
+    const uint8_t* gate_scale;
+    const void* up;
+    const uint8_t* up_scale;
+    const void* down;
+    const uint8_t* down_scale;
+} moe_fp4_experts_t;
+
+/* Workspace that is enough for any of the three calls below and any call of moe_query's list (host only). */
+int moe_query_fp4(const moe_desc_t* desc, size_t* workspace_bytes);
+
+/*
+ * moe_grouped_ffn, moe_dispatch_ffn and moe_layer_forward with 4-bit experts.  desc->dtype is MOE_DTYPE_BF16 (the type of xp / x,
+ * yp and y); any other is MOE_ERR_UNSUPPORTED.  d is a multiple of 8, h any number; both at most 2^21.
+ * The rows that the experts read are x in 4 bits: with x_scale == NULL, x is bf16 and is quantised on the way; otherwise x holds
+ * 4-bit rows, as moe_norm_rows or moe_quantize_rows_fp4 leave them, and x_scale their scales.  The layer's router always reads bf16,
+ * x; xq and xq_scale, both or neither, are the same rows in 4 bits.  The hidden activation is rounded to bf16 once, then to 4 bits.
+ * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp4 and moe_layer_forward_fp4: N * d < 2^31; all three:
+ * P_max < 2^31 and max(P_max, N) * ceil(max(d, h) / 512) < 2^31; else MOE_ERR_UNSUPPORTED.  Where no row can survive (P_max = 0)
+ * nothing is enqueued for the FFN, and x, xp, row_token and yp may be null.
+ * Where the quantising of x is a launch of its own, a profile table counts it as MOE_KERNEL_DISPATCH.
+ */
+int moe_grouped_ffn_fp4(const moe_desc_t* desc, const void* xp, const uint8_t* xp_scale, const int32_t* expert_offset,
+                        const moe_fp4_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes,
+                        void* stream);
+int moe_dispatch_ffn_fp4(const moe_desc_t* desc, const void* x, const uint8_t* x_scale, const int32_t* expert_offset,
+                         const int32_t* row_token, const moe_fp4_experts_t* experts, void* yp, void* workspace,
+                         size_t workspace_bytes, void* stream);
+int moe_layer_forward_fp4(const moe_desc_t* desc, const void* x, const void* xq, const uint8_t* xq_scale, const float* w_router,
+                          const float* bias, const moe_fp4_experts_t* experts, const uint8_t* token_class, uint32_t seed,
+                          float* logits, float* scores, int32_t* topk_idx, float* topk_score, int32_t* expert_count,
+                          int32_t* seg_count, int32_t* expert_offset, int32_t* row_token, float* row_weight,
+                          int32_t* pair_row, void* yp, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Profiling hook (instrumentation, not part of the method).  The table is the caller's (host memory); the
  * library keeps only a pointer to it, per host thread, between moe_profile_attach(table) and
  * moe_profile_attach(NULL).  While a table is attached to the calling thread, every launch of kernel id k by

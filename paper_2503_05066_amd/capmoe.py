@@ -45,6 +45,19 @@ class MoeFp8Experts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "gate_scale", "up", "up_scale", "down", "down_scale")]
 
 
+class MoeNorm(ctypes.Structure):
+    """moe_norm_t of include/capmoe.h."""
+
+    _fields_ = [("n_rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("bits", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class MoeFp4Experts(ctypes.Structure):
+    """moe_fp4_experts_t of include/capmoe.h."""
+
+    _fields_ = MoeFp8Experts._fields_
+
+
 KERNELS = ("router_logits", "softmax_topk", "drop_prepare", "drop_select", "drop_emit", "dispatch", "ffn_schedule",
            "ffn_gate_up", "ffn_down", "combine", "drop_limit")
 
@@ -116,6 +129,20 @@ def load():
         lib.moe_grouped_ffn_fp8.argtypes = [dp, vp, vp, ep, vp, vp, sz, vp]
         lib.moe_dispatch_ffn_fp8.argtypes = [dp, vp, vp, vp, ep, vp, vp, sz, vp]
         lib.moe_layer_forward_fp8.argtypes = [dp, vp, vp, vp, ep, vp, ctypes.c_uint32] + [vp] * 13 + [sz, vp]
+        ep4 = ctypes.POINTER(MoeFp4Experts)
+        lib.moe_fp4_query.argtypes = lib.moe_fp8_query.argtypes
+        lib.moe_quantize_rows_fp4.argtypes = lib.moe_quantize_rows.argtypes
+        lib.moe_quantize_weights_fp4.argtypes = lib.moe_quantize_weights.argtypes
+        lib.moe_dequantize_rows.argtypes = [i32, i32, vp, vp, i64, ctypes.c_int32, vp, vp]
+        lib.moe_norm_rows.argtypes = [ctypes.POINTER(MoeNorm)] + [vp] * 9
+        lib.moe_grouped_gemm_fp4.argtypes = [gp] + [vp] * 8
+        lib.moe_query_fp4.argtypes = [dp, ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_grouped_ffn_fp4.argtypes = [dp, vp, vp, vp, ep4, vp, vp, sz, vp]
+        lib.moe_dispatch_ffn_fp4.argtypes = [dp, vp, vp, vp, vp, ep4, vp, vp, sz, vp]
+        lib.moe_layer_forward_fp4.argtypes = [dp, vp, vp, vp, vp, vp, ep4, vp, ctypes.c_uint32] + [vp] * 13 + [sz, vp]
+        for f in ("moe_fp4_query", "moe_quantize_rows_fp4", "moe_quantize_weights_fp4", "moe_dequantize_rows", "moe_norm_rows",
+                  "moe_grouped_gemm_fp4", "moe_query_fp4", "moe_grouped_ffn_fp4", "moe_dispatch_ffn_fp4", "moe_layer_forward_fp4"):
+            getattr(lib, f).restype = i32
         for f in ("moe_fp8_query", "moe_quantize_rows", "moe_quantize_weights", "moe_gemm_query", "moe_grouped_gemm_fp8",
                   "moe_query_fp8", "moe_grouped_ffn_fp8", "moe_dispatch_ffn_fp8", "moe_layer_forward_fp8"):
             getattr(lib, f).restype = i32
@@ -285,13 +312,7 @@ def _fits_fp8(t, shape, what):
 _fp8_pitches = functools.lru_cache(maxsize=256)(lambda cols: moe_fp8_query(cols))
 
 
-def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
-    """x [*, cols] (bf16 or fp32) into the 8-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
-    dtype = _value_dtype(x, 2, "x")
-    n_rows, cols = q.shape[0], x.shape[1]
-    pitch, scale_pitch = _fp8_pitches(cols)
-    _fits_fp8(q, (n_rows, pitch), "q")
-    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+def _fits_row_source(x, row_token, row_count, n_rows):
     if row_token is None:
         _fits(x.shape[0] >= n_rows, "x: a row for every row of q")
     else:
@@ -299,6 +320,16 @@ def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
               "row_token: a dense int32 for every row of q")
     if row_count is not None:
         _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
+
+
+def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
+    """x [*, cols] (bf16 or fp32) into the 8-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
+    dtype = _value_dtype(x, 2, "x")
+    n_rows, cols = q.shape[0], x.shape[1]
+    pitch, scale_pitch = _fp8_pitches(cols)
+    _fits_fp8(q, (n_rows, pitch), "q")
+    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+    _fits_row_source(x, row_token, row_count, n_rows)
     _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
                                     _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows")
 
@@ -393,11 +424,11 @@ def _product_sizes(gemm: bytes):
     return sizes.max_rows, sizes.src_rows, 4 * (sizes.n_experts + 1), sizes.n_out, pitch, scale_pitch, w, w_bytes, w_scale_bytes
 
 
-def _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
+def _fits_product(sizes, x, x_scale, row_token, expert_offset, w, w_scale, y):
     """False if there are no rows, else every tensor against the sizes of the call.  (Of rows that are not gathered, x holds as
     many as expert_offset ends with, known on the device only.)  In one expression, 1.2 us: one by one the checks took 2 us more, of
     8 for a token's experts."""
-    max_rows, src_rows, offset_bytes, n_out, pitch, scale_pitch, w_shape, w_bytes, w_scale_bytes = _product_sizes(bytes(gemm))
+    max_rows, src_rows, offset_bytes, n_out, pitch, scale_pitch, w_shape, w_bytes, w_scale_bytes = sizes
     if max_rows == 0:
         return False
     bf16, int32 = _product_dtypes()
@@ -423,7 +454,7 @@ def _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
 def moe_grouped_gemm_fp8(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, workspace, stream=None):
     """workspace may be None where moe_gemm_query answers 0.  A tensor that does not fit the sizes of gemm is refused."""
     arrays = (None,) * 7  # without rows none is read
-    if _fits_product(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y):
+    if _fits_product(_product_sizes(bytes(gemm)), x, x_scale, row_token, expert_offset, w, w_scale, y):
         arrays = (x.data_ptr(), x_scale.data_ptr(), None if row_token is None else row_token.data_ptr(), expert_offset.data_ptr(),
                   w.data_ptr(), w_scale.data_ptr(), y.data_ptr())
     _check(load().moe_grouped_gemm_fp8(ctypes.byref(gemm), *arrays, _ptr(workspace),
@@ -465,6 +496,207 @@ def moe_layer_forward_fp8(desc, x, w_router, bias, experts: Fp8Experts, token_cl
     return buf.y
 
 
+def moe_fp4_query(cols: int):
+    """(pitch, scale_pitch) in bytes of a 4-bit matrix of this many columns; host only."""
+    pitch, scale_pitch = ctypes.c_int32(), ctypes.c_int32()
+    _check(load().moe_fp4_query(int(cols), ctypes.byref(pitch), ctypes.byref(scale_pitch)), "moe_fp4_query")
+    return pitch.value, scale_pitch.value
+
+
+_fp4_pitches = functools.lru_cache(maxsize=256)(lambda cols: moe_fp4_query(cols))
+
+
+def fp4_row_buffers(n_rows: int, cols: int, device="cuda"):
+    """(values, scales) of the 4-bit form of [n_rows, cols], uninitialised."""
+    import torch
+
+    pitch, scale_pitch = moe_fp4_query(cols)
+    return (torch.empty((n_rows, pitch), dtype=torch.uint8, device=device),
+            torch.empty((n_rows, scale_pitch), dtype=torch.uint8, device=device))
+
+
+def fp4_weight_buffers(n_experts: int, n_out: int, n_in: int, device="cuda"):
+    """(values, scales) of the 4-bit form of expert weights [n_experts, n_out, n_in], uninitialised."""
+    import torch
+
+    pitch, scale_pitch = moe_fp4_query(n_in)
+    rows = -(-n_out // 128) * 128
+    return (torch.empty((n_experts, rows, pitch), dtype=torch.uint8, device=device),
+            torch.empty((n_experts, rows, scale_pitch), dtype=torch.uint8, device=device))
+
+
+def moe_quantize_rows_fp4(x, row_token, row_count, q, scale, stream=None):
+    """x [*, cols] (bf16 or fp32) into the 4-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
+    dtype = _value_dtype(x, 2, "x")
+    n_rows, cols = q.shape[0], x.shape[1]
+    pitch, scale_pitch = _fp4_pitches(cols)
+    _fits_fp8(q, (n_rows, pitch), "q")
+    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+    _fits_row_source(x, row_token, row_count, n_rows)
+    _check(load().moe_quantize_rows_fp4(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
+                                        _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows_fp4")
+
+
+def moe_quantize_weights_fp4(w, q, scale, stream=None):
+    """w [E, n_out, n_in] (bf16 or fp32) into the 4-bit weights q, scale (see fp4_weight_buffers)."""
+    dtype = _value_dtype(w, 3, "w")
+    e, n_out, n_in = w.shape
+    pitch, scale_pitch = _fp4_pitches(n_in)
+    rows = -(-n_out // 128) * 128
+    _fits_fp8(q, (e, rows, pitch), "q")
+    _fits_fp8(scale, (e, rows, scale_pitch), "scale")
+    _check(load().moe_quantize_weights_fp4(dtype, _ptr(w), e, n_out, n_in, _ptr(q), _ptr(scale), _stream_on(stream, w, q, scale)),
+           "moe_quantize_weights_fp4")
+
+
+def moe_dequantize_rows(bits, q, scale, y, stream=None):
+    """The values of the 4- or 8-bit rows q, scale into y [n_rows, cols] (bf16 or fp32)."""
+    dtype = _value_dtype(y, 2, "y")
+    n_rows, cols = y.shape
+    pitch, scale_pitch = _fp8_pitches(cols) if bits == 8 else _fp4_pitches(cols)
+    _fits_fp8(q, (n_rows, pitch), "q")
+    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+    _check(load().moe_dequantize_rows(int(bits), dtype, _ptr(q), _ptr(scale), n_rows, cols, _ptr(y), _stream_on(stream, q, scale, y)),
+           "moe_dequantize_rows")
+
+
+def make_norm(n_rows, cols, eps=1e-6, dtype=DTYPE_BF16, bits=0) -> MoeNorm:
+    return MoeNorm(n_rows, cols, dtype, bits, eps)
+
+
+def moe_norm_rows(norm, x, residual, weight, row_count, sum, y, q, scale, stream=None):
+    """See include/capmoe.h.  residual, weight, row_count, sum may be None, y too where q and scale (with norm.bits) are given."""
+    n_rows, cols, bits = norm.n_rows, norm.cols, norm.bits
+    shape = (n_rows, cols)
+    for t, dims, want, what in ((x, 2, shape, "x"), (residual, 2, shape, "residual"), (weight, 1, (cols,), "weight"), (sum, 2, shape, "sum"),
+                                (y, 2, shape, "y")):
+        if t is not None and (_value_dtype(t, dims, what) != norm.dtype or t.shape != want):
+            raise ValueError(f"{what}: of the norm's type and {want}")
+    if bits and q is not None and scale is not None:
+        pitch, scale_pitch = _fp8_pitches(cols) if bits == 8 else _fp4_pitches(cols)
+        _fits_fp8(q, (n_rows, pitch), "q")
+        _fits_fp8(scale, (n_rows, scale_pitch), "scale")
+    if row_count is not None:
+        _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
+    _check(load().moe_norm_rows(ctypes.byref(norm), _ptr(x), _ptr(residual), _ptr(weight), _ptr(row_count), _ptr(sum), _ptr(y), _ptr(q),
+                                _ptr(scale), _stream_on(stream, x, residual, weight, row_count, sum, y, q, scale)), "moe_norm_rows")
+
+
+class Fp4Experts:
+    """The 4-bit weights of a layer's experts (keeps the tensors alive; allocation and marshalling only)."""
+
+    def __init__(self, gate, gate_scale, up, up_scale, down, down_scale):
+        if gate.dim() != 3 or down.dim() != 3:
+            raise ValueError("4-bit expert weights have three dimensions")
+        e, h, d = gate.shape[0], gate.shape[1], down.shape[1]  # filled up to multiples of 128
+        for q, scale, n, k in ((gate, gate_scale, h, d), (up, up_scale, h, d), (down, down_scale, d, h)):
+            pitch, scale_pitch = _fp4_pitches(k)
+            if tuple(q.shape) != (e, n, pitch) or n % 128 or q.element_size() != 1 or not q.is_contiguous():
+                raise ValueError(f"4-bit expert weights {tuple(q.shape)}: expected {(e, n, pitch)}, rows a multiple of 128, one byte, contiguous")
+            if tuple(scale.shape) != (e, n, scale_pitch) or scale.element_size() != 1 or not scale.is_contiguous():
+                raise ValueError(f"scales {tuple(scale.shape)} of expert weights {(e, n, pitch)}")
+            if q.device != gate.device or scale.device != gate.device:
+                raise ValueError("4-bit expert weights on more than one device")
+        self.sizes = (e, h, d)
+        self.tensors = (gate, gate_scale, up, up_scale, down, down_scale)
+        self.struct = MoeFp4Experts(*[t.data_ptr() for t in self.tensors])
+
+    def of(self, desc: MoeDesc):
+        """The struct for a call of that layer."""
+        if self.sizes != (desc.n_experts, -(-desc.d_hidden // 128) * 128, -(-desc.d_model // 128) * 128):
+            raise ValueError(f"4-bit experts of {self.sizes} do not belong to this layer")
+        return ctypes.byref(self.struct)
+
+    @classmethod
+    def quantized(cls, w_gate, w_up, w_down, stream=None):
+        """From w_gate, w_up [E,h,d] and w_down [E,d,h] in bf16 or fp32 (as at model load).  The tensors belong to `stream`:
+        work on others that uses them waits for it."""
+        import torch
+
+        tensors = []
+        with torch.cuda.stream(stream):  # their memory too: what another stream gave back, its work may still write
+            for w in (w_gate, w_up, w_down):
+                q, scale = fp4_weight_buffers(*w.shape, device=w.device)
+                moe_quantize_weights_fp4(w, q, scale, stream)
+                tensors += [q, scale]
+        return cls(*tensors)
+
+
+@functools.lru_cache(maxsize=256)
+def _product_sizes_fp4(gemm: bytes):
+    """The fields of a MoeGemm that the call accepts, and what they say of the tensors."""
+    sizes = MoeGemm.from_buffer_copy(gemm)
+    moe_gemm_query(sizes)  # refuses sizes that the call refuses
+    pitch, scale_pitch = moe_fp4_query(sizes.n_in)
+    w = (sizes.n_experts, -(-sizes.n_out // 128) * 128, pitch)
+    return sizes.max_rows, sizes.src_rows, 4 * (sizes.n_experts + 1), sizes.n_out, pitch, scale_pitch, w, math.prod(w), w[0] * w[1] * scale_pitch
+
+
+def moe_grouped_gemm_fp4(gemm, x, x_scale, row_token, expert_offset, w, w_scale, y, stream=None):
+    """A tensor that does not fit the sizes of gemm is refused."""
+    arrays = (None,) * 7  # without rows none is read
+    if _fits_product(_product_sizes_fp4(bytes(gemm)), x, x_scale, row_token, expert_offset, w, w_scale, y):
+        arrays = (x.data_ptr(), x_scale.data_ptr(), None if row_token is None else row_token.data_ptr(), expert_offset.data_ptr(),
+                  w.data_ptr(), w_scale.data_ptr(), y.data_ptr())
+    _check(load().moe_grouped_gemm_fp4(ctypes.byref(gemm), *arrays,
+                                       _stream_on(stream, x, x_scale, row_token, expert_offset, w, w_scale, y)), "moe_grouped_gemm_fp4")
+
+
+def moe_query_fp4(desc: MoeDesc) -> int:
+    """Workspace bytes of a layer with 4-bit experts; host only."""
+    ws = ctypes.c_size_t()
+    _check(load().moe_query_fp4(ctypes.byref(desc), ctypes.byref(ws)), "moe_query_fp4")
+    return ws.value
+
+
+def _fits_ffn_fp4(desc, x, x_scale, rows, what):
+    """x with its scales in 4 bits, or bf16 without."""
+    if x is None:
+        return
+    if x_scale is None:
+        _fits(_value_dtype(x, 2, what) == DTYPE_BF16 and x.shape[0] >= rows and x.shape[1] == desc.d_model, f"{what}: bf16 [*, d_model], or scales")
+    else:
+        pitch, scale_pitch = _fp4_pitches(desc.d_model)
+        _fits(x.dim() == 2 and x.shape[0] >= rows, f"{what}: a row for every one that the call may read")
+        _fits_fp8(x, (x.shape[0], pitch), what)
+        _fits_fp8(x_scale, (x.shape[0], scale_pitch), what + "'s scales")
+
+
+def moe_grouped_ffn_fp4(desc, xp, xp_scale, expert_offset, experts: Fp4Experts, yp, workspace, stream=None):
+    """xp: bf16 rows with xp_scale None, or 4-bit rows with their scales."""
+    _fits_ffn_fp4(desc, xp, xp_scale, 0, "xp")  # of its rows only those of the plan are read
+    _check(load().moe_grouped_ffn_fp4(ctypes.byref(desc), _ptr(xp), _ptr(xp_scale), _ptr(expert_offset), experts.of(desc),
+                                      _ptr(yp), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream_on(stream, xp, xp_scale, expert_offset, yp, workspace, experts.tensors[0])),
+           "moe_grouped_ffn_fp4")
+
+
+def moe_dispatch_ffn_fp4(desc, x, x_scale, expert_offset, row_token, experts: Fp4Experts, yp, workspace, stream=None):
+    """x: bf16 tokens with x_scale None, or 4-bit rows with their scales."""
+    _fits_ffn_fp4(desc, x, x_scale, desc.n_tokens, "x")
+    _check(load().moe_dispatch_ffn_fp4(ctypes.byref(desc), _ptr(x), _ptr(x_scale), _ptr(expert_offset), _ptr(row_token),
+                                       experts.of(desc), _ptr(yp), _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(),
+                                       _stream_on(stream, x, x_scale, expert_offset, row_token, yp, workspace, experts.tensors[0])),
+           "moe_dispatch_ffn_fp4")
+
+
+def moe_layer_forward_fp4(desc, x, xq, xq_scale, w_router, bias, experts: Fp4Experts, token_class, seed, buf, stream=None):
+    """The whole layer with 4-bit experts, into the buffers of a LayerBuffers made with fp4=True.  xq, xq_scale: x in 4 bits, or
+    None."""
+    ws = buf.workspace
+    if xq is not None and xq_scale is not None:
+        _fits_ffn_fp4(desc, xq, xq_scale, desc.n_tokens, "xq")
+    _check(load().moe_layer_forward_fp4(
+        ctypes.byref(desc), _ptr(x), _ptr(xq), _ptr(xq_scale), _ptr(w_router), _ptr(bias), experts.of(desc), _ptr(token_class),
+        int(seed) & 0xFFFFFFFF, _ptr(buf.logits), _ptr(buf.scores), _ptr(buf.topk_idx), _ptr(buf.topk_score),
+        _ptr(buf.expert_count), _ptr(buf.seg_count), _ptr(buf.expert_offset), _ptr(buf.row_token),
+        _ptr(buf.row_weight), _ptr(buf.pair_row), _ptr(buf.yp), _ptr(buf.y), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream_on(stream, x, xq, xq_scale, w_router, bias, token_class, ws, experts.tensors[0])),
+        "moe_layer_forward_fp4")
+    return buf.y
+
+
 def moe_profile_attach(table: "MoeProfile | None"):
     """Attach the caller's profile table to this thread (None detaches).  The caller keeps the table alive."""
     _check(load().moe_profile_attach(ctypes.byref(table) if table is not None else None), "moe_profile_attach")
@@ -493,13 +725,15 @@ def moe_probe_mfma_bf16(blocks: int, iterations: int, sink, random_operands: boo
 class LayerBuffers:
     """Device buffers of one layer call, sized by moe_query (allocation only, no arithmetic)."""
 
-    def __init__(self, desc: MoeDesc, device="cuda", fp8=False):
+    def __init__(self, desc: MoeDesc, device="cuda", fp8=False, fp4=False):
         import torch
 
         self.desc = desc
         self.cap, self.slots, self.max_rows, self.workspace_bytes = moe_query(desc)
         if fp8:  # for the calls with 8-bit experts as well
             self.workspace_bytes = moe_query_fp8(desc)
+        if fp4:  # .. with 4-bit experts
+            self.workspace_bytes = max(self.workspace_bytes, moe_query_fp4(desc))
         n, e, k, d = desc.n_tokens, desc.n_experts, desc.top_k + desc.overselect, desc.d_model
         blocks = desc.device_groups if desc.capacity_scope in (SCOPE_LOCAL, SCOPE_LOCAL_DEVICE) else 1
         act = torch.bfloat16 if desc.dtype == DTYPE_BF16 else torch.float32

@@ -1,0 +1,262 @@
+// The entry points of the norm and of the 4-bit experts: argument validation, workspace layout, the calls' launches.
+#include <algorithm>
+
+#include "fp4.h"
+
+namespace capmoe {
+
+static bool misaligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+// Workspace of a layer's FFN.  (A product by itself needs none.)
+struct Fp4Workspace {
+    void* hidden;  // [P_max, h filled up to a multiple of 128] bf16
+    void* hq;      // .. in 4 bits
+    uint8_t* hs;
+    void* xq;      // [rows of x, pitch]
+    uint8_t* xs;
+    size_t bytes;
+};
+
+static Fp4Workspace ffn_fp4_workspace(const moe_desc_t& d, const Sizes& s, void* base) {
+    Fp4Workspace w;
+    char* p = (char*)base;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        void* at = p + off;
+        off += align256(bytes);
+        return at;
+    };
+    const int64_t rows = std::max<int64_t>(s.max_rows, 1), x_rows = std::max<int64_t>(rows, d.n_tokens);
+    w.hidden = take((size_t)rows * fp8_pitch(d.d_hidden) * 2);
+    w.hq = take((size_t)rows * fp4_pitch(d.d_hidden));
+    w.hs = (uint8_t*)take((size_t)rows * fp4_scale_pitch(d.d_hidden));
+    w.xq = take((size_t)x_rows * fp4_pitch(d.d_model));
+    w.xs = (uint8_t*)take((size_t)x_rows * fp4_scale_pitch(d.d_model));
+    w.bytes = off;
+    return w;
+}
+
+static int validate_gemm4(const moe_gemm_t* g) {
+    if (!g || g->max_rows < 0 || g->src_rows < 0 || g->n_experts < 1 || g->n_in < 1 || g->n_out < 1) return MOE_ERR_INVALID_ARG;
+    if (g->n_experts > kMaxExperts || g->n_in > kFp8MaxWidth || g->n_out > kFp8MaxWidth || g->n_out % 8 != 0) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+static int validate_fp4(const moe_desc_t* d) {
+    const int v = validate(d);
+    if (v != MOE_OK) return v;
+    if (d->dtype != MOE_DTYPE_BF16 || d->d_model % 8 != 0 || d->d_model > kFp8MaxWidth || d->d_hidden > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    const int64_t rows = derive(*d).max_rows, groups = fp4_groups(std::max(d->d_model, d->d_hidden));
+    if (rows >= (int64_t)1 << 31 || std::max<int64_t>(rows, d->n_tokens) * groups >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+// The first product addresses all of x, as bf16 or as 4-bit rows, through one window of 4 GiB.
+static bool too_large_to_gather(const moe_desc_t* d) { return (uint64_t)d->n_tokens * (uint64_t)d->d_model >= (1ull << 31); }
+
+static int validate_experts4(const moe_fp4_experts_t* w) {
+    if (!w || !w->gate || !w->gate_scale || !w->up || !w->up_scale || !w->down || !w->down_scale) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {w->gate, w->up, w->down, (const void*)w->gate_scale, (const void*)w->up_scale, (const void*)w->down_scale})
+        if (misaligned(p, 16)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+// The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows; x_scale == nullptr: they are bf16.
+static hipError_t launch_ffn_fp4(const moe_desc_t& d, const Sizes& s, const Fp4Workspace& ws, const void* x, const uint8_t* x_scale,
+                                 const int32_t* row_token, const int32_t* expert_offset, const moe_fp4_experts_t& w, void* yp,
+                                 hipStream_t st) {
+    const int hp = fp8_pitch(d.d_hidden);
+    const Fp4Gemm up = fp4_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp4_gemm(d.n_experts, s.max_rows, d.d_hidden, d.d_model);
+    const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
+    if (!x_scale) {
+        ProfileScope prof(MOE_KERNEL_DISPATCH, st);
+        const hipError_t e = launch_quantize_rows_fp4(MOE_DTYPE_BF16, x, x_rows, d.d_model, nullptr,
+                                                      row_token ? nullptr : expert_offset + d.n_experts, ws.xq, ws.xs, st);
+        if (e != hipSuccess) return e;
+        x = ws.xq, x_scale = ws.xs;
+    }
+    {
+        ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
+        launch_fp4_product(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, st);
+        const hipError_t e = launch_quantize_rows_fp4(MOE_DTYPE_BF16, ws.hidden, s.max_rows, hp, nullptr, expert_offset + d.n_experts, ws.hq,
+                                                      ws.hs, st);
+        if (e != hipSuccess) return e;
+    }
+    ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
+    launch_fp4_product(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, st);
+    return hipGetLastError();
+}
+
+}  // namespace capmoe
+
+using namespace capmoe;
+
+static int ffn_fp4_impl(const moe_desc_t* desc, const void* x, const uint8_t* x_scale, const int32_t* row_token,
+                        const int32_t* expert_offset, const moe_fp4_experts_t* experts, void* yp, const Fp4Workspace& ws, void* stream) {
+    return launch_ffn_fp4(*desc, derive(*desc), ws, x, x_scale, row_token, expert_offset, *experts, yp, (hipStream_t)stream) == hipSuccess
+               ? MOE_OK
+               : MOE_ERR_HIP;
+}
+
+static int ffn_fp4_checked(const moe_desc_t* desc, const void* x, const uint8_t* x_scale, bool gathered, const int32_t* row_token,
+                           const int32_t* expert_offset, const moe_fp4_experts_t* experts, void* yp, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    const int v = validate_fp4(desc);
+    if (v != MOE_OK) return v;
+    const Sizes s = derive(*desc);
+    if (!expert_offset || !workspace || (s.max_rows > 0 && (!x || !yp || (gathered && !row_token)))) return MOE_ERR_INVALID_ARG;
+    if (misaligned(x, 16) || misaligned(x_scale, 16) || misaligned(yp, 16) || misaligned(workspace, 256)) return MOE_ERR_INVALID_ARG;
+    const int w = validate_experts4(experts);
+    if (w != MOE_OK) return w;
+    if (gathered && too_large_to_gather(desc)) return MOE_ERR_UNSUPPORTED;
+    const Fp4Workspace ws = ffn_fp4_workspace(*desc, s, workspace);
+    if (workspace_bytes < ws.bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    if (s.max_rows == 0) return MOE_OK;
+    return ffn_fp4_impl(desc, x, x_scale, row_token, expert_offset, experts, yp, ws, stream);
+}
+
+// Whether rows of `cols` values are moved in 16-byte pieces.
+static int row_checks(int dtype, int64_t n_rows, int32_t cols) {
+    if ((dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16) || cols < 1 || n_rows < 0) return MOE_ERR_INVALID_ARG;
+    if (cols > kFp8MaxWidth || cols % (dtype == MOE_DTYPE_BF16 ? 8 : 4) != 0) return MOE_ERR_UNSUPPORTED;
+    if (n_rows >= (int64_t)1 << 31 || n_rows * fp4_groups(cols) >= (int64_t)1 << 31) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+extern "C" {
+
+int moe_norm_rows(const moe_norm_t* norm, const void* x, const void* residual, const void* weight, const int32_t* row_count,
+                  void* sum, void* y, void* q, uint8_t* scale, void* stream) {
+    if (!norm) return MOE_ERR_INVALID_ARG;
+    const int v = row_checks(norm->dtype, norm->n_rows, norm->cols);
+    if (v != MOE_OK) return v;
+    if (norm->bits != 0 && norm->bits != 4 && norm->bits != 8) return MOE_ERR_INVALID_ARG;
+    if (!(norm->eps >= 0x1p-126f) || norm->eps > 0x1.fffffep127f) return MOE_ERR_INVALID_ARG;
+    if (norm->n_rows == 0) return MOE_OK;
+    if (!x || (!y && norm->bits == 0) || (norm->bits != 0 && (!q || !scale))) return MOE_ERR_INVALID_ARG;
+    if (sum && sum == y) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, residual, weight, (const void*)sum, (const void*)y})
+        if (misaligned(p, 16)) return MOE_ERR_INVALID_ARG;
+    if (norm->bits != 0 && (misaligned(q, 16) || misaligned(scale, norm->bits == 4 ? 16 : 4))) return MOE_ERR_INVALID_ARG;
+    return launch_norm_rows(*norm, x, residual, weight, row_count, sum, y, q, scale, (hipStream_t)stream) == hipSuccess ? MOE_OK
+                                                                                                                        : MOE_ERR_HIP;
+}
+
+int moe_fp4_query(int32_t cols, int32_t* pitch, int32_t* scale_pitch) {
+    if (cols < 1) return MOE_ERR_INVALID_ARG;
+    if (cols > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (pitch) *pitch = fp4_pitch(cols);
+    if (scale_pitch) *scale_pitch = fp4_scale_pitch(cols);
+    return MOE_OK;
+}
+
+int moe_quantize_rows_fp4(int dtype, const void* x, int64_t n_rows, int32_t cols, const int32_t* row_token,
+                          const int32_t* row_count, void* q, uint8_t* scale, void* stream) {
+    const int v = row_checks(dtype, n_rows, cols);
+    if (v != MOE_OK) return v;
+    if (n_rows == 0) return MOE_OK;
+    if (!x || !q || !scale || misaligned(x, 16) || misaligned(q, 16) || misaligned(scale, 16)) return MOE_ERR_INVALID_ARG;
+    return launch_quantize_rows_fp4(dtype, x, n_rows, cols, row_token, row_count, q, scale, (hipStream_t)stream) == hipSuccess
+               ? MOE_OK
+               : MOE_ERR_HIP;
+}
+
+int moe_quantize_weights_fp4(int dtype, const void* w, int32_t n_experts, int32_t n_out, int32_t n_in, void* q, uint8_t* scale,
+                             void* stream) {
+    if (n_experts < 1 || n_out < 1) return MOE_ERR_INVALID_ARG;
+    if (n_out > kFp8MaxWidth) return MOE_ERR_UNSUPPORTED;
+    const int v = row_checks(dtype, (int64_t)n_experts * fp8_pitch(n_out), n_in);
+    if (v != MOE_OK) return v;
+    if (!w || !q || !scale || misaligned(w, 16) || misaligned(q, 16) || misaligned(scale, 16)) return MOE_ERR_INVALID_ARG;
+    return launch_quantize_weights_fp4(dtype, w, n_experts, n_out, n_in, q, scale, (hipStream_t)stream) == hipSuccess ? MOE_OK
+                                                                                                                       : MOE_ERR_HIP;
+}
+
+int moe_dequantize_rows(int bits, int dtype, const void* q, const uint8_t* scale, int64_t n_rows, int32_t cols, void* y, void* stream) {
+    if (bits != 4 && bits != 8) return MOE_ERR_INVALID_ARG;
+    const int v = row_checks(dtype, n_rows, cols);
+    if (v != MOE_OK) return v;
+    if (n_rows == 0) return MOE_OK;
+    if (!q || !scale || !y || misaligned(q, 16) || misaligned(scale, bits == 4 ? 16 : 4) || misaligned(y, 16)) return MOE_ERR_INVALID_ARG;
+    return launch_dequantize_rows(bits, dtype, q, scale, n_rows, cols, y, (hipStream_t)stream) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+int moe_grouped_gemm_fp4(const moe_gemm_t* gemm, const void* x, const uint8_t* x_scale, const int32_t* row_token,
+                         const int32_t* expert_offset, const void* w, const uint8_t* w_scale, void* y, void* stream) {
+    const int v = validate_gemm4(gemm);
+    if (v != MOE_OK) return v;
+    if (gemm->max_rows == 0) return MOE_OK;
+    if (!x || !x_scale || !expert_offset || !w || !w_scale || !y) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, (const void*)x_scale, w, (const void*)w_scale, (const void*)y})
+        if (misaligned(p, 16)) return MOE_ERR_INVALID_ARG;
+    const Fp4Gemm g = fp4_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
+    if (row_token && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
+    if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
+    launch_fp4_product(g, expert_offset, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
+                       (hipStream_t)stream);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+int moe_query_fp4(const moe_desc_t* desc, size_t* workspace_bytes) {
+    const int v = validate_fp4(desc);
+    if (v != MOE_OK) return v;
+    size_t other = 0;
+    const int q = moe_query(desc, nullptr, nullptr, nullptr, &other);
+    if (q != MOE_OK) return q;
+    const size_t mine = ffn_fp4_workspace(*desc, derive(*desc), nullptr).bytes;
+    if (workspace_bytes) *workspace_bytes = std::max(mine, other);
+    return MOE_OK;
+}
+
+int moe_grouped_ffn_fp4(const moe_desc_t* desc, const void* xp, const uint8_t* xp_scale, const int32_t* expert_offset,
+                        const moe_fp4_experts_t* experts, void* yp, void* workspace, size_t workspace_bytes, void* stream) {
+    return ffn_fp4_checked(desc, xp, xp_scale, false, nullptr, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+}
+
+int moe_dispatch_ffn_fp4(const moe_desc_t* desc, const void* x, const uint8_t* x_scale, const int32_t* expert_offset,
+                         const int32_t* row_token, const moe_fp4_experts_t* experts, void* yp, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    return ffn_fp4_checked(desc, x, x_scale, true, row_token, expert_offset, experts, yp, workspace, workspace_bytes, stream);
+}
+
+int moe_layer_forward_fp4(const moe_desc_t* desc, const void* x, const void* xq, const uint8_t* xq_scale, const float* w_router,
+                          const float* bias, const moe_fp4_experts_t* experts, const uint8_t* token_class, uint32_t seed,
+                          float* logits, float* scores, int32_t* topk_idx, float* topk_score, int32_t* expert_count,
+                          int32_t* seg_count, int32_t* expert_offset, int32_t* row_token, float* row_weight, int32_t* pair_row,
+                          void* yp, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    // every check first, so that a refusal leaves nothing enqueued
+    const int v = validate_fp4(desc);
+    if (v != MOE_OK) return v;
+    const Sizes s = derive(*desc);
+    if (!expert_count || !seg_count || !expert_offset || !workspace) return MOE_ERR_INVALID_ARG;
+    if (misaligned(workspace, 256) || (xq == nullptr) != (xq_scale == nullptr)) return MOE_ERR_INVALID_ARG;
+    if (desc->n_tokens > 0) {
+        if (!x || !w_router || !logits || !scores || !topk_idx || !topk_score || !pair_row || !yp || !y || !row_weight)
+            return MOE_ERR_INVALID_ARG;
+        for (const void* p : {x, xq, (const void*)xq_scale, (const void*)w_router, (const void*)yp, (const void*)y, (const void*)scores,
+                              (const void*)topk_idx, (const void*)pair_row})
+            if (misaligned(p, 16)) return MOE_ERR_INVALID_ARG;
+        if (too_large_to_gather(desc)) return MOE_ERR_UNSUPPORTED;
+    }
+    if (s.max_rows > 0) {
+        if (!row_token) return MOE_ERR_INVALID_ARG;
+        const int w = validate_experts4(experts);
+        if (w != MOE_OK) return w;
+    }
+    size_t need = 0;
+    const int q = moe_query_fp4(desc, &need);
+    if (q != MOE_OK) return q;
+    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    int st = moe_route_topk(desc, x, w_router, bias, 0, logits, scores, topk_idx, topk_score, workspace, workspace_bytes, stream);
+    if (st != MOE_OK) return st;
+    st = moe_capacity_drop_ranked(desc, scores, topk_idx, token_class, seed, expert_count, seg_count, expert_offset, row_token,
+                                  row_weight, pair_row, workspace, workspace_bytes, stream);
+    if (st != MOE_OK) return st;
+    if (s.max_rows > 0) {
+        st = ffn_fp4_impl(desc, xq ? xq : x, xq_scale, row_token, expert_offset, experts, yp, ffn_fp4_workspace(*desc, s, workspace), stream);
+        if (st != MOE_OK) return st;
+    }
+    return moe_combine(desc, yp, row_weight, pair_row, y, stream);
+}
+
+}  // extern "C"

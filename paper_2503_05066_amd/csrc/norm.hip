@@ -1,0 +1,279 @@
+// The residual's addition and the root-mean-square norm of rows, with the rows also in 8 or 4 bits:
+//
+//   h = round(x + residual),  y = round(h / sqrt(mean(h^2) + eps) * weight),  q = the 8- or 4-bit form of y
+//
+// One pass over the data: a row stays in the registers of its waves (rows of more than kNormMostColumns are read twice).  The
+// sum of squares is fp32: a lane adds its values in ascending order, then the lanes, then the waves, always in the same order.
+#include <algorithm>
+
+#include "ffn_tile.h"
+#include "fp4.h"
+
+namespace capmoe {
+
+constexpr int kNormMostColumns = 16 * 4 * kFp4Group;  // 16 waves with four groups of 512 columns each
+
+struct NormArgs {
+    const void *x, *residual, *weight;
+    const int32_t* row_count;
+    void *sum, *y;
+    uint8_t *q, *scale;
+    int64_t n_rows;
+    int cols, bits;
+    float eps;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void floats(const Eight<BF16>& e, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        f[i] = BF16 ? __uint_as_float(i & 1 ? e.v[i / 2] & 0xffff0000u : e.v[i / 2] << 16) : __uint_as_float(e.v[i % (BF16 ? 4 : 8)]);
+}
+template <bool BF16>
+__device__ __forceinline__ Eight<BF16> rounded(const float (&f)[8]) {
+    Eight<BF16> e;
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 4 : 8); ++i) e.v[i] = BF16 ? pack_bf16x2(f[(2 * i) % 8], f[(2 * i + 1) % 8]) : __float_as_uint(f[i]);
+    return e;
+}
+template <bool BF16>
+__device__ __forceinline__ void store(const Eight<BF16>& e, void* row, int col, int cols) {
+    if constexpr (BF16) {
+        if (col < cols) *(uint4*)((uint16_t*)row + col) = make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]);
+    } else {
+        if (col < cols) *(uint4*)((float*)row + col) = make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]);
+        if (col + 4 < cols) *(uint4*)((float*)row + col + 4) = make_uint4(e.v[4], e.v[5], e.v[6], e.v[7]);
+    }
+}
+
+// The 8-bit form of a wave's 512 columns (see write_group_fp4).
+template <bool BF16>
+__device__ __forceinline__ void write_group_fp8(Eight<BF16> e, int lane, int col, int cols_filled, uint8_t* q, uint8_t* scale) {
+    uint32_t bad;
+    const uint32_t byte = scale_byte(max_of_16(e.amax(bad)));
+    if (col < cols_filled) *(uint2*)(q + lane * 8) = e.quantized(byte, bad);
+    const uint32_t word = or_over_rows_of_16(byte << (8 * (lane >> 4)));
+    if (lane == 0) *(uint32_t*)scale = word;
+}
+
+__device__ __forceinline__ float sum_of_wave(float v) {
+    auto add = [&](int other) { v += __int_as_float(other); };
+    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));   // lane ^ 1
+    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));   // lane ^ 2
+    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));  // the other quad of eight lanes
+    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));  // the other eight of sixteen
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = __int_as_float((int)a[0]) + __int_as_float((int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return __int_as_float((int)b[0]) + __int_as_float((int)b[1]);
+}
+
+// 1 / sqrt(mean + eps) from the sum of squares of h * shrink
+__device__ __forceinline__ float inverse_root(float squares, int cols, float eps, float shrink) {
+    return rsqrtf(squares / (float)cols + eps * shrink * shrink) * shrink;
+}
+// What a row's values are multiplied by where their squares pass the range of fp32: the least of them that then counts is far above
+// what gets lost.
+constexpr float kNormShrink = 0x1p-80f;
+
+// the sum over the waves of a row, in the order of the waves
+template <int WAVES>
+__device__ __forceinline__ float sum_of_row(float v, float* part, int wave) {
+    v = sum_of_wave(v);
+    if constexpr (WAVES > 1) {
+        __syncthreads();  // the sums before have been read
+        if ((threadIdx.x & 63) == 0) part[wave] = v;
+        __syncthreads();
+        v = 0.f;
+        const int first = wave / WAVES * WAVES;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) v += part[first + i];
+    }
+    return v;
+}
+
+template <bool BF16>
+__device__ __forceinline__ Eight<BF16> with_residual(const NormArgs& p, const Eight<BF16>& x, const Eight<BF16>& r) {
+    float a[8], b[8];
+    floats(x, a), floats(r, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] += b[i];
+    return rounded<BF16>(a);
+}
+
+// a group's outputs
+template <bool BF16>
+__device__ __forceinline__ void write_normed(const NormArgs& p, const Eight<BF16>& h, const Eight<BF16>& w, float inverse, int64_t row,
+                                             int group, int lane) {
+    const int col = group * kFp4Group + lane * 8;
+    float f[8], g[8];
+    floats(h, f), floats(w, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= inverse;
+    if (p.weight) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= g[i];
+    }
+    Eight<BF16> y = rounded<BF16>(f);
+    if (p.y) store(y, (uint8_t*)p.y + row * p.cols * (BF16 ? 2 : 4), col, p.cols);
+    if (!p.bits) return;
+    if (inverse != inverse) {  // behind the row's end, where 0 * NaN is not 0
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col + i >= p.cols) f[i] = 0.f;
+        y = rounded<BF16>(f);
+    }
+    if (p.bits == 4) {
+        const int filled = fp4_slabs(p.cols) * kFp4Slab;
+        write_group_fp4(y, lane, col, filled, p.q + row * (filled / 2) + group * (kFp4Group / 2),
+                        p.scale + row * fp4_scale_pitch(p.cols) + group * 16);
+    } else {
+        const int filled = fp8_pitch(p.cols);
+        write_group_fp8(y, lane, col, filled, p.q + row * filled + group * kFp4Group, p.scale + row * fp8_scale_pitch(p.cols) + group * 4);
+    }
+}
+
+// WAVES waves take a row, GROUPS groups of 512 columns each.
+template <bool BF16, int WAVES, int GROUPS>
+__global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel(const NormArgs p) {
+    constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;  // of a block
+    __shared__ float part[WAVES < 4 ? 4 : WAVES];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, of_row = wave % WAVES;
+    const int64_t row = (int64_t)blockIdx.x * kRows + wave / WAVES;
+    const int64_t n_rows = p.row_count ? min(p.n_rows, (int64_t)max(*p.row_count, 0)) : p.n_rows;
+    const bool valid = row < n_rows;
+    if (kRows == 1 && !valid) return;
+    const int64_t at = row * p.cols * (BF16 ? 2 : 4);
+    const int end = valid ? p.cols : 0;
+    Eight<BF16> h[GROUPS], w[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) h[i].load((const uint8_t*)p.x + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
+    if (p.residual) {
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) w[i].load((const uint8_t*)p.residual + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) h[i] = with_residual(p, h[i], w[i]);
+    }
+    if (p.weight) {
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) w[i].load(p.weight, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
+    }
+    float squares = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        float f[8];
+        floats(h[i], f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(f[k], f[k], squares);
+    }
+    squares = sum_of_row<WAVES>(squares, part, wave);
+    float inverse = inverse_root(squares, p.cols, p.eps, 1.0f);
+    const bool large = !(squares < __builtin_inff());
+    if (WAVES == 1 || kRows == 1 ? large : __syncthreads_or(large)) {  // rare
+        float small = 0.f;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            float f[8];
+            floats(h[i], f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) small = __builtin_fmaf(f[k] * kNormShrink, f[k] * kNormShrink, small);
+        }
+        small = sum_of_row<WAVES>(small, part, wave);
+        if (large) inverse = inverse_root(small, p.cols, p.eps, kNormShrink);
+    }
+    if (!valid) return;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        const int group = i * WAVES + of_row;
+        if (group * kFp4Group >= p.cols) continue;
+        if (p.sum) store(h[i], (uint8_t*)p.sum + at, group * kFp4Group + lane * 8, p.cols);
+        write_normed(p, h[i], w[i], inverse, row, group, lane);
+    }
+}
+
+// Rows that no registers hold: sixteen waves read them twice.  (sum may be x or the residual, so the second time it is read.)
+template <bool BF16>
+__global__ __launch_bounds__(1024) void norm_long_rows_kernel(const NormArgs p) {
+    __shared__ float part[16];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t row = blockIdx.x;
+    if (p.row_count && row >= *p.row_count) return;
+    const int64_t at = row * p.cols * (BF16 ? 2 : 4);
+    const int groups = fp4_groups(p.cols);
+    auto load = [&](int col, bool first) {
+        Eight<BF16> h;
+        if (!first && p.sum) {
+            h.load((const uint8_t*)p.sum + at, col, p.cols);
+            return h;
+        }
+        h.load((const uint8_t*)p.x + at, col, p.cols);
+        if (p.residual) {
+            Eight<BF16> r;
+            r.load((const uint8_t*)p.residual + at, col, p.cols);
+            h = with_residual(p, h, r);
+        }
+        return h;
+    };
+    auto squares_of = [&](float shrink, bool first) {
+        float squares = 0.f;
+        for (int g = wave; g < groups; g += 16) {
+            const int col = g * kFp4Group + lane * 8;
+            const Eight<BF16> h = load(col, first);
+            if (first && p.sum) store(h, (uint8_t*)p.sum + at, col, p.cols);
+            float f[8];
+            floats(h, f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(f[k] * shrink, f[k] * shrink, squares);
+        }
+        return sum_of_row<16>(squares, part, wave);
+    };
+    const float squares = squares_of(1.0f, true);
+    float inverse = inverse_root(squares, p.cols, p.eps, 1.0f);
+    if (!(squares < __builtin_inff())) inverse = inverse_root(squares_of(kNormShrink, false), p.cols, p.eps, kNormShrink);
+    for (int g = wave; g < groups; g += 16) {
+        const int col = g * kFp4Group + lane * 8;
+        const Eight<BF16> h = load(col, false);
+        Eight<BF16> w;
+        if (p.weight) w.load(p.weight, col, p.cols);
+        write_normed(p, h, w, inverse, row, g, lane);
+    }
+}
+
+template <bool BF16>
+static void launch_norm(const NormArgs& p, hipStream_t st) {
+    const int groups = fp4_groups(p.cols);
+    auto launch = [&](auto kern, int waves) {
+        const int rows = waves < 4 ? 4 / waves : 1;
+        hipLaunchKernelGGL(kern, dim3((unsigned)((p.n_rows + rows - 1) / rows)), dim3(64 * std::max(waves, 4)), 0, st, p);
+    };
+    if (groups == 1)
+        launch(norm_rows_kernel<BF16, 1, 1>, 1);
+    else if (groups == 2)
+        launch(norm_rows_kernel<BF16, 2, 1>, 2);
+    else if (groups <= 4)
+        launch(norm_rows_kernel<BF16, 4, 1>, 4);
+    else if (groups <= 8)
+        launch(norm_rows_kernel<BF16, 4, 2>, 4);
+    else if (groups <= 16)
+        launch(norm_rows_kernel<BF16, 4, 4>, 4);
+    else if (groups <= 32)
+        launch(norm_rows_kernel<BF16, 8, 4>, 8);
+    else if (p.cols <= kNormMostColumns)
+        launch(norm_rows_kernel<BF16, 16, 4>, 16);
+    else
+        launch(norm_long_rows_kernel<BF16>, 16);
+}
+
+hipError_t launch_norm_rows(const moe_norm_t& norm, const void* x, const void* residual, const void* weight,
+                            const int32_t* row_count, void* sum, void* y, void* q, uint8_t* scale, hipStream_t st) {
+    NormArgs p;
+    p.x = x, p.residual = residual, p.weight = weight, p.row_count = row_count, p.sum = sum, p.y = y;
+    p.q = (uint8_t*)q, p.scale = scale, p.n_rows = norm.n_rows, p.cols = norm.cols, p.bits = norm.bits, p.eps = norm.eps;
+    if (norm.dtype == MOE_DTYPE_BF16)
+        launch_norm<true>(p, st);
+    else
+        launch_norm<false>(p, st);
+    return hipGetLastError();
+}
+
+}  // namespace capmoe
