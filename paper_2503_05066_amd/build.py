@@ -20,7 +20,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libcapmoe.so")
 
 SOURCES = ["api.hip", "route.hip", "router_mfma.hip", "drop.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip", "probe.hip",
-           "quantize.hip", "fp8.hip", "fp8_thin.hip", "api_fp8.hip", "norm.hip", "quantize_fp4.hip", "fp4.hip", "api_fp4.hip"]
+           "quantize.hip", "fp8.hip", "fp8_thin.hip", "api_fp8.hip", "norm.hip", "quantize_fp4.hip", "fp4.hip", "fp4_thin.hip",
+           "api_fp4.hip"]
 # the packed-fp32 feature is switched off for all device code; the first sixteen words of a kernel's arguments arrive in
 # registers (a token through 64 experts x 2048 x 1024: 38.3 -> 37.7 us); the router file must not contract
 # multiplies and adds (its softmax is a fixed sequence of individually rounded operations)
@@ -29,9 +30,9 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", os.path.j
           "-Wno-unused-command-line-argument"]
 PER_FILE = {"route.hip": ["-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt"]}
 # sources whose asm statements name accumulation registers: the assembly of the same compilation is checked
-NAMED_ACCUMULATORS = {"ffn.hip", "fp8.hip"}
+NAMED_ACCUMULATORS = {"ffn.hip", "fp8.hip", "fp4.hip"}
 # a source that is compiled in parts, an object each
-PARTS = {"fp8.hip": [["-DCAPMOE_FP8_SHAPE=%d" % i] for i in range(3)]}
+PARTS = {"fp8.hip": [["-DCAPMOE_FP8_SHAPE=%d" % i] for i in range(3)], "fp4.hip": [["-DCAPMOE_FP4_SHAPE=%d" % i] for i in range(3)]}
 
 
 def _hipcc() -> str:

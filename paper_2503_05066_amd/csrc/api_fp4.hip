@@ -61,12 +61,35 @@ static int validate_experts4(const moe_fp4_experts_t* w) {
     return MOE_OK;
 }
 
+// One product on high row tiles (fp4.hip).
+static void launch_fp4_tiles(const Fp4Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
+                             const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up, const uint8_t* up_scale,
+                             void* y, uint8_t* y_scale, bool stream, hipStream_t st) {
+    Fp4Args p;
+    p.x = (const uint8_t*)x, p.x_scale = x_scale, p.x_rows = x_rows, p.gather = gather;
+    p.w[0] = (const uint8_t*)w, p.w[1] = (const uint8_t*)up;
+    p.w_scale[0] = w_scale, p.w_scale[1] = up_scale;
+    p.y = (uint8_t*)y, p.y_scale = y_scale;
+    p.expert_offset = expert_offset, p.max_rows = g.max_rows, p.experts = g.experts;
+    p.pitch = g.pitch, p.scale_pitch = g.scale_pitch;
+    p.n = g.n, p.n_pad = g.n_pad, p.y_pitch = fp4_pitch(g.n), p.y_scale_pitch = fp4_scale_pitch(g.n);
+    p.col_group = p.tile_shift = 0;
+    p.stream = stream;
+    if (up)
+        launch_fp4_shape<256, true>(p, st);
+    else if (fp4_tiles_are_wide(g, compute_units()))
+        launch_fp4_shape<256, false>(p, st);
+    else
+        launch_fp4_shape<128, false>(p, st);
+}
+
 // The FFN behind the argument checks.  row_token == nullptr: x holds the permuted rows; x_scale == nullptr: they are bf16.
 static hipError_t launch_ffn_fp4(const moe_desc_t& d, const Sizes& s, const Fp4Workspace& ws, const void* x, const uint8_t* x_scale,
                                  const int32_t* row_token, const int32_t* expert_offset, const moe_fp4_experts_t& w, void* yp,
                                  hipStream_t st) {
     const int hp = fp8_pitch(d.d_hidden);
-    const Fp4Gemm up = fp4_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp4_gemm(d.n_experts, s.max_rows, d.d_hidden, d.d_model);
+    const Fp4Gemm up = fp4_gemm(d.n_experts, s.max_rows, d.d_model, hp), down = fp4_gemm(d.n_experts, s.max_rows, hp, d.d_model);
+    const bool stream = fp8_weights_stream(3.0 * d.n_experts * up.pitch * up.n_pad);
     const int64_t x_rows = row_token ? d.n_tokens : s.max_rows;
     if (!x_scale) {
         ProfileScope prof(MOE_KERNEL_DISPATCH, st);
@@ -75,15 +98,24 @@ static hipError_t launch_ffn_fp4(const moe_desc_t& d, const Sizes& s, const Fp4W
         if (e != hipSuccess) return e;
         x = ws.xq, x_scale = ws.xs;
     }
+    if (!fp4_ffn_is_few_rows(d, s)) {
+        {
+            ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
+            launch_fp4_tiles(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hq, ws.hs, stream, st);
+        }
+        ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
+        launch_fp4_tiles(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr, stream, st);
+        return hipGetLastError();
+    }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-        launch_fp4_product(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, st);
+        launch_fp4_thin(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, st);
         const hipError_t e = launch_quantize_rows_fp4(MOE_DTYPE_BF16, ws.hidden, s.max_rows, hp, nullptr, expert_offset + d.n_experts, ws.hq,
                                                       ws.hs, st);
         if (e != hipSuccess) return e;
     }
     ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-    launch_fp4_product(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, st);
+    launch_fp4_thin(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, st);
     return hipGetLastError();
 }
 
@@ -192,8 +224,12 @@ int moe_grouped_gemm_fp4(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     const Fp4Gemm g = fp4_gemm(gemm->n_experts, gemm->max_rows, gemm->n_in, gemm->n_out);
     if (row_token && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
-    launch_fp4_product(g, expert_offset, x, x_scale, row_token ? gemm->src_rows : gemm->max_rows, row_token, w, w_scale, nullptr, nullptr, y,
-                       (hipStream_t)stream);
+    const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
+    if (fp4_gemm_is_few_rows(g))
+        launch_fp4_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, (hipStream_t)stream);
+    else
+        launch_fp4_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr,
+                         fp8_weights_stream((double)g.experts * g.pitch * g.n_pad), (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

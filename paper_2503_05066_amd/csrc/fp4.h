@@ -94,9 +94,18 @@ hipError_t launch_dequantize_rows(int bits, int dtype, const void* q, const uint
 hipError_t launch_norm_rows(const moe_norm_t& norm, const void* x, const void* residual, const void* weight,
                             const int32_t* row_count, void* sum, void* y, void* q, uint8_t* scale, hipStream_t st);
 
-// A product on 4-bit rows, or the gate and the up product with y = silu(gate) * up (then w_up != nullptr); y is bf16 of g.n columns.
-void launch_fp4_product(const Fp4Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
-                        const int32_t* gather, const void* w, const uint8_t* w_scale, const void* w_up, const uint8_t* up_scale,
-                        void* y, hipStream_t st);
+// Arguments of the kernels for high row tiles (fp4.hip): as those of the 8-bit ones (fp8.h); y: bf16 rows of n columns, with SWIGLU 4-bit
+// rows of y_pitch bytes.
+struct Fp4Args : Fp8Args {
+    int y_pitch;
+};
+template <int BN, bool SWIGLU>
+void launch_fp4_shape(Fp4Args p, hipStream_t st);
+
+// Kernels for tiles of few rows.  A product on 4-bit rows, or the gate and the up product with y = silu(gate) * up (then w_up != nullptr);
+// y is bf16 of g.n columns.
+void launch_fp4_thin(const Fp4Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
+                     const int32_t* gather, const void* w, const uint8_t* w_scale, const void* w_up, const uint8_t* up_scale,
+                     void* y, hipStream_t st);
 
 }  // namespace capmoe
