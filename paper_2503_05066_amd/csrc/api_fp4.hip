@@ -9,10 +9,9 @@ static bool misaligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes
 
 // Workspace of a layer's FFN.  (A product by itself needs none.)
 struct Fp4Workspace {
-    void* hidden;  // [P_max, h filled up to a multiple of 128] bf16
-    void* hq;      // .. in 4 bits
+    void* hq;     // [P_max, pitch of h]: the hidden activation
     uint8_t* hs;
-    void* xq;      // [rows of x, pitch]
+    void* xq;     // [rows of x, pitch of d]
     uint8_t* xs;
     size_t bytes;
 };
@@ -27,7 +26,6 @@ static Fp4Workspace ffn_fp4_workspace(const moe_desc_t& d, const Sizes& s, void*
         return at;
     };
     const int64_t rows = std::max<int64_t>(s.max_rows, 1), x_rows = std::max<int64_t>(rows, d.n_tokens);
-    w.hidden = take((size_t)rows * fp8_pitch(d.d_hidden) * 2);
     w.hq = take((size_t)rows * fp4_pitch(d.d_hidden));
     w.hs = (uint8_t*)take((size_t)rows * fp4_scale_pitch(d.d_hidden));
     w.xq = take((size_t)x_rows * fp4_pitch(d.d_model));
@@ -109,13 +107,10 @@ static hipError_t launch_ffn_fp4(const moe_desc_t& d, const Sizes& s, const Fp4W
     }
     {
         ProfileScope prof(MOE_KERNEL_FFN_GATE_UP, st);
-        launch_fp4_thin(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hidden, st);
-        const hipError_t e = launch_quantize_rows_fp4(MOE_DTYPE_BF16, ws.hidden, s.max_rows, hp, nullptr, expert_offset + d.n_experts, ws.hq,
-                                                      ws.hs, st);
-        if (e != hipSuccess) return e;
+        launch_fp4_thin(up, expert_offset, x, x_scale, x_rows, row_token, w.gate, w.gate_scale, w.up, w.up_scale, ws.hq, ws.hs, stream, st);
     }
     ProfileScope prof(MOE_KERNEL_FFN_DOWN, st);
-    launch_fp4_thin(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, st);
+    launch_fp4_thin(down, expert_offset, ws.hq, ws.hs, s.max_rows, nullptr, w.down, w.down_scale, nullptr, nullptr, yp, nullptr, stream, st);
     return hipGetLastError();
 }
 
@@ -225,11 +220,13 @@ int moe_grouped_gemm_fp4(const moe_gemm_t* gemm, const void* x, const uint8_t* x
     if (row_token && gemm->src_rows == 0) return MOE_ERR_INVALID_ARG;
     if (row_token && (uint64_t)gemm->src_rows * (uint64_t)g.pitch > kBeyond) return MOE_ERR_UNSUPPORTED;
     const int64_t x_rows = row_token ? gemm->src_rows : gemm->max_rows;
+    const bool streamed = fp8_weights_stream((double)g.experts * g.pitch * g.n_pad);
     if (fp4_gemm_is_few_rows(g))
-        launch_fp4_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, (hipStream_t)stream);
+        launch_fp4_thin(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed,
+                        (hipStream_t)stream);
     else
-        launch_fp4_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr,
-                         fp8_weights_stream((double)g.experts * g.pitch * g.n_pad), (hipStream_t)stream);
+        launch_fp4_tiles(g, expert_offset, x, x_scale, x_rows, row_token, w, w_scale, nullptr, nullptr, y, nullptr, streamed,
+                         (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -102,10 +102,10 @@ struct Fp4Args : Fp8Args {
 template <int BN, bool SWIGLU>
 void launch_fp4_shape(Fp4Args p, hipStream_t st);
 
-// Kernels for tiles of few rows.  A product on 4-bit rows, or the gate and the up product with y = silu(gate) * up (then w_up != nullptr);
-// y is bf16 of g.n columns.
+// Kernels for tiles of few rows: a product, y bf16, or (up != nullptr) the gate and the up product and y, y_scale = silu(gate) * up in
+// 4 bits; g.n is then a multiple of 128.
 void launch_fp4_thin(const Fp4Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,
-                     const int32_t* gather, const void* w, const uint8_t* w_scale, const void* w_up, const uint8_t* up_scale,
-                     void* y, hipStream_t st);
+                     const int32_t* gather, const void* w, const uint8_t* w_scale, const void* up, const uint8_t* up_scale, void* y,
+                     uint8_t* y_scale, bool stream, hipStream_t st);
 
 }  // namespace capmoe

@@ -11,8 +11,8 @@
 // would cost their launches.  Nor is there a tile schedule: a block finds its expert in the offsets.
 #include <algorithm>
 
-#include "ffn_tile.h"
 #include "fp8.h"
+#include "narrow_tile.h"
 
 namespace capmoe {
 
@@ -265,40 +265,6 @@ struct Thin8 {
                 }
             }
         }
-    }
-};
-
-// The t-th expert that has rows: its id and rows, or false.  Every wave looks it up for itself.
-struct ExpertRows {
-    int e, row0, rows;
-    int lo[kMaxExperts / kWave], hi[kMaxExperts / kWave];
-    __device__ __forceinline__ ExpertRows(const int32_t* offset, int experts) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int c = 0; c < kMaxExperts / kWave; ++c) {
-            const int i = c * kWave + lane;
-            lo[c] = i < experts ? offset[i] : 0;
-            hi[c] = i < experts ? offset[i + 1] : 0;
-        }
-    }
-    __device__ __forceinline__ bool find(int t) {
-        bool found = false;
-#pragma unroll
-        for (int c = 0; c < kMaxExperts / kWave; ++c) {
-            const uint64_t has = __ballot(hi[c] > lo[c]);
-            const int n = __popcll(has);
-            if (!found && t < n) {
-                const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-                const uint64_t it = __ballot(hi[c] > lo[c] && rank == t);
-                const int at = __builtin_ctzll(it);
-                e = c * kWave + at;
-                row0 = __builtin_amdgcn_readlane(lo[c], at);
-                rows = __builtin_amdgcn_readlane(hi[c], at) - row0;
-                found = true;
-            }
-            t -= n;
-        }
-        return found;
     }
 };
 

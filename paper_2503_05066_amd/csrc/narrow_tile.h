@@ -1,4 +1,5 @@
-// What the products on 8-bit and on 4-bit rows share on high row tiles (fp8.hip, fp4.hip): the order of the work and the bf16 output.
+// What the products on 8-bit and on 4-bit rows share: on high row tiles (fp8.hip, fp4.hip) the order of the work and the bf16 output, on
+// few rows (fp8_thin.hip, fp4_thin.hip) the experts that have any.
 #pragma once
 
 #include "ffn_tile.h"
@@ -196,6 +197,40 @@ struct TileOrder {
             ++round;
         } while (more && !w.valid);
         return w;
+    }
+};
+
+// The t-th expert that has rows: its id and rows, or false.  Every wave looks it up for itself.
+struct ExpertRows {
+    int e, row0, rows;
+    int lo[kMaxExperts / kWave], hi[kMaxExperts / kWave];
+    __device__ __forceinline__ ExpertRows(const int32_t* offset, int experts) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int c = 0; c < kMaxExperts / kWave; ++c) {
+            const int i = c * kWave + lane;
+            lo[c] = i < experts ? offset[i] : 0;
+            hi[c] = i < experts ? offset[i + 1] : 0;
+        }
+    }
+    __device__ __forceinline__ bool find(int t) {
+        bool found = false;
+#pragma unroll
+        for (int c = 0; c < kMaxExperts / kWave; ++c) {
+            const uint64_t has = __ballot(hi[c] > lo[c]);
+            const int n = __popcll(has);
+            if (!found && t < n) {
+                const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+                const uint64_t it = __ballot(hi[c] > lo[c] && rank == t);
+                const int at = __builtin_ctzll(it);
+                e = c * kWave + at;
+                row0 = __builtin_amdgcn_readlane(lo[c], at);
+                rows = __builtin_amdgcn_readlane(hi[c], at) - row0;
+                found = true;
+            }
+            t -= n;
+        }
+        return found;
     }
 };
 
