@@ -312,16 +312,6 @@ def _fits_fp8(t, shape, what):
 _fp8_pitches = functools.lru_cache(maxsize=256)(lambda cols: moe_fp8_query(cols))
 
 
-def _fits_row_source(x, row_token, row_count, n_rows):
-    if row_token is None:
-        _fits(x.shape[0] >= n_rows, "x: a row for every row of q")
-    else:
-        _fits(row_token.dtype == _value_dtypes["int32"] and row_token.numel() >= n_rows and row_token.is_contiguous(),
-              "row_token: a dense int32 for every row of q")
-    if row_count is not None:
-        _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
-
-
 def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
     """x [*, cols] (bf16 or fp32) into the 8-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
     dtype = _value_dtype(x, 2, "x")
@@ -329,7 +319,13 @@ def moe_quantize_rows(x, row_token, row_count, q, scale, stream=None):
     pitch, scale_pitch = _fp8_pitches(cols)
     _fits_fp8(q, (n_rows, pitch), "q")
     _fits_fp8(scale, (n_rows, scale_pitch), "scale")
-    _fits_row_source(x, row_token, row_count, n_rows)
+    if row_token is None:
+        _fits(x.shape[0] >= n_rows, "x: a row for every row of q")
+    else:
+        _fits(row_token.dtype == _value_dtypes["int32"] and row_token.numel() >= n_rows and row_token.is_contiguous(),
+              "row_token: a dense int32 for every row of q")
+    if row_count is not None:
+        _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
     _check(load().moe_quantize_rows(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
                                     _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows")
 
@@ -525,15 +521,32 @@ def fp4_weight_buffers(n_experts: int, n_out: int, n_in: int, device="cuda"):
             torch.empty((n_experts, rows, scale_pitch), dtype=torch.uint8, device=device))
 
 
+@functools.lru_cache(maxsize=None)
+def _row_dtypes():
+    """The types of rows of values, by what the calls name them, and of row numbers."""
+    import torch
+
+    return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}, torch.int32
+
+
 def moe_quantize_rows_fp4(x, row_token, row_count, q, scale, stream=None):
     """x [*, cols] (bf16 or fp32) into the 4-bit rows q [n_rows, pitch], scale [n_rows, scale_pitch]."""
-    dtype = _value_dtype(x, 2, "x")
-    n_rows, cols = q.shape[0], x.shape[1]
-    pitch, scale_pitch = _fp4_pitches(cols)
-    _fits_fp8(q, (n_rows, pitch), "q")
-    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
-    _fits_row_source(x, row_token, row_count, n_rows)
-    _check(load().moe_quantize_rows_fp4(dtype, _ptr(x), n_rows, cols, _ptr(row_token), _ptr(row_count), _ptr(q), _ptr(scale),
+    dtypes, int32 = _row_dtypes()
+    try:  # in one expression (see _fits_product)
+        (rows, cols), (n_rows, q_cols) = x.shape, q.shape
+        dtype = dtypes[x.dtype]
+        pitch, scale_pitch = _fp4_pitches(cols)
+        fits = (x.is_contiguous() and q_cols == pitch and q.nbytes == n_rows * pitch and q.is_contiguous() and
+                scale.shape == (n_rows, scale_pitch) and scale.nbytes == n_rows * scale_pitch and scale.is_contiguous() and
+                (rows >= n_rows if row_token is None else
+                 row_token.dtype is int32 and row_token.nbytes >= 4 * n_rows and row_token.is_contiguous()) and
+                (row_count is None or row_count.dtype is int32 and row_count.nbytes >= 4))
+    except (AttributeError, KeyError, ValueError):  # no tensor, of another type, or not of two dimensions
+        fits = False
+    if not fits:
+        raise ValueError("rows in 4 bits: dense tensors x bf16 or fp32 [*, cols], a row for every one of q or row_token int32 for each, "
+                         "row_count int32, q and scale of the bytes that moe_fp4_query says")
+    _check(load().moe_quantize_rows_fp4(dtype, x.data_ptr(), n_rows, cols, _ptr(row_token), _ptr(row_count), q.data_ptr(), scale.data_ptr(),
                                         _stream_on(stream, x, row_token, row_count, q, scale)), "moe_quantize_rows_fp4")
 
 
@@ -551,34 +564,52 @@ def moe_quantize_weights_fp4(w, q, scale, stream=None):
 
 def moe_dequantize_rows(bits, q, scale, y, stream=None):
     """The values of the 4- or 8-bit rows q, scale into y [n_rows, cols] (bf16 or fp32)."""
-    dtype = _value_dtype(y, 2, "y")
-    n_rows, cols = y.shape
-    pitch, scale_pitch = _fp8_pitches(cols) if bits == 8 else _fp4_pitches(cols)
-    _fits_fp8(q, (n_rows, pitch), "q")
-    _fits_fp8(scale, (n_rows, scale_pitch), "scale")
-    _check(load().moe_dequantize_rows(int(bits), dtype, _ptr(q), _ptr(scale), n_rows, cols, _ptr(y), _stream_on(stream, q, scale, y)),
-           "moe_dequantize_rows")
+    dtypes, _ = _row_dtypes()
+    try:
+        n_rows, cols = y.shape
+        dtype = dtypes[y.dtype]
+        pitch, scale_pitch = _fp8_pitches(cols) if bits == 8 else _fp4_pitches(cols)
+        fits = (y.is_contiguous() and q.shape == (n_rows, pitch) and q.nbytes == n_rows * pitch and q.is_contiguous() and
+                scale.shape == (n_rows, scale_pitch) and scale.nbytes == n_rows * scale_pitch and scale.is_contiguous())
+    except (AttributeError, KeyError, ValueError):
+        fits = False
+    if not fits:
+        raise ValueError("values of rows: dense tensors y bf16 or fp32 [n_rows, cols], q and scale of the bytes that the format has for them")
+    _check(load().moe_dequantize_rows(int(bits), dtype, q.data_ptr(), scale.data_ptr(), n_rows, cols, y.data_ptr(),
+                                      _stream_on(stream, q, scale, y)), "moe_dequantize_rows")
 
 
 def make_norm(n_rows, cols, eps=1e-6, dtype=DTYPE_BF16, bits=0) -> MoeNorm:
     return MoeNorm(n_rows, cols, dtype, bits, eps)
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_sizes(norm: bytes):
+    """What a MoeNorm says of the tensors: type, shape, the weight's shape, shapes and bytes of q and scale."""
+    n = MoeNorm.from_buffer_copy(norm)
+    dtype = {value: key for key, value in _row_dtypes()[0].items()}.get(n.dtype)
+    pitch, scale_pitch = {4: moe_fp4_query, 8: moe_fp8_query}[n.bits](n.cols) if n.bits in (4, 8) else (0, 0)
+    return dtype, (n.n_rows, n.cols), (n.cols,), (n.n_rows, pitch), n.n_rows * pitch, (n.n_rows, scale_pitch), n.n_rows * scale_pitch
+
+
 def moe_norm_rows(norm, x, residual, weight, row_count, sum, y, q, scale, stream=None):
     """See include/capmoe.h.  residual, weight, row_count, sum may be None, y too where q and scale (with norm.bits) are given."""
-    n_rows, cols, bits = norm.n_rows, norm.cols, norm.bits
-    shape = (n_rows, cols)
-    for t, dims, want, what in ((x, 2, shape, "x"), (residual, 2, shape, "residual"), (weight, 1, (cols,), "weight"), (sum, 2, shape, "sum"),
-                                (y, 2, shape, "y")):
-        if t is not None and (_value_dtype(t, dims, what) != norm.dtype or t.shape != want):
-            raise ValueError(f"{what}: of the norm's type and {want}")
-    if bits and q is not None and scale is not None:
-        pitch, scale_pitch = _fp8_pitches(cols) if bits == 8 else _fp4_pitches(cols)
-        _fits_fp8(q, (n_rows, pitch), "q")
-        _fits_fp8(scale, (n_rows, scale_pitch), "scale")
-    if row_count is not None:
-        _fits(row_count.dtype == _value_dtypes["int32"] and row_count.numel() > 0, "row_count: an int32")
-    _check(load().moe_norm_rows(ctypes.byref(norm), _ptr(x), _ptr(residual), _ptr(weight), _ptr(row_count), _ptr(sum), _ptr(y), _ptr(q),
+    dtype, shape, width, q_shape, q_bytes, scale_shape, scale_bytes = _norm_sizes(bytes(norm))
+    try:
+        fits = (x.dtype is dtype and x.shape == shape and x.is_contiguous() and
+                (residual is None or residual.dtype is dtype and residual.shape == shape and residual.is_contiguous()) and
+                (weight is None or weight.dtype is dtype and weight.shape == width and weight.is_contiguous()) and
+                (sum is None or sum.dtype is dtype and sum.shape == shape and sum.is_contiguous()) and
+                (y is None or y.dtype is dtype and y.shape == shape and y.is_contiguous()) and
+                (q is None or not q_bytes or q.shape == q_shape and q.nbytes == q_bytes and q.is_contiguous()) and
+                (scale is None or not q_bytes or scale.shape == scale_shape and scale.nbytes == scale_bytes and scale.is_contiguous()) and
+                (row_count is None or row_count.dtype is _row_dtypes()[1] and row_count.nbytes >= 4))
+    except AttributeError:  # no tensor
+        fits = False
+    if not fits:
+        raise ValueError(f"a norm of {shape} takes dense tensors of its type: x, residual, sum, y {list(shape)}, weight {list(width)}; q bytes "
+                         f"{list(q_shape)}, scale bytes {list(scale_shape)}, row_count int32")
+    _check(load().moe_norm_rows(ctypes.byref(norm), x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(row_count), _ptr(sum), _ptr(y), _ptr(q),
                                 _ptr(scale), _stream_on(stream, x, residual, weight, row_count, sum, y, q, scale)), "moe_norm_rows")
 
 

@@ -7,7 +7,7 @@
 // the row's 512 k around it (of every second slab from the L2: what a ring holds then has one form).
 //
 // The hidden activation leaves in 4 bits: 32 of its columns share a scale, which two neighbouring waves hold, so they exchange the
-// largest magnitudes of their rows; eight waves make a block, so that also four to a weight row leave two neighbours in it.
+// largest magnitudes of their rows; with four waves to a weight row eight make a block, so that it has two neighbours.
 #include <algorithm>
 
 #include "fp4.h"
@@ -278,12 +278,12 @@ struct Thin4 {
 
 // The blocks take the experts in turn; one with more rows than a pass holds is done in passes over the same weights, which are
 // then fetched to be kept.
-template <bool SWIGLU, bool STREAM>
-__global__ __launch_bounds__(SWIGLU ? 512 : 256, 2) void fp4_thin_kernel(const Thin4Args p) {
+template <bool SWIGLU, bool STREAM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void fp4_thin_kernel(const Thin4Args p) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    constexpr int kWaves = SWIGLU ? 8 : 4, kMost = 32;  // rows of a pass
+    constexpr int kMost = 32;  // rows of a pass
     ExpertRows x(p.expert_offset, p.experts);
-    const int first = blockIdx.x / p.col_blocks, n0 = (blockIdx.x - first * p.col_blocks) * (kWaves / p.split) * Thin4<16, SWIGLU, STREAM>::kCols;
+    const int first = blockIdx.x / p.col_blocks, n0 = (blockIdx.x - first * p.col_blocks) * (WAVES / p.split) * Thin4<16, SWIGLU, STREAM>::kCols;
     const int step = gridDim.x / p.col_blocks;
     for (int t = first; x.find(t); t += step) {
         for (int at = 0; at < x.rows; at += kMost) {
@@ -300,19 +300,26 @@ __global__ __launch_bounds__(SWIGLU ? 512 : 256, 2) void fp4_thin_kernel(const T
     }
 }
 
-template <bool SWIGLU, bool STREAM>
-static void launch_thin4(Thin4Args a, int64_t tiles, hipStream_t st) {
-    constexpr int waves = SWIGLU ? 8 : 4, lds = waves * kThin4RingBytes;
-    auto kern = fp4_thin_kernel<SWIGLU, STREAM>;
+template <bool SWIGLU, bool STREAM, int WAVES>
+static void launch_thin4_waves(Thin4Args a, int64_t tiles, hipStream_t st) {
+    constexpr int lds = WAVES * kThin4RingBytes;
+    auto kern = fp4_thin_kernel<SWIGLU, STREAM, WAVES>;
     static std::atomic<uint64_t> configured{0};
     once_per_device(configured, [&] {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     });
+    const int per_block = WAVES / a.split * Thin4<16, SWIGLU, STREAM>::kCols;
+    a.col_blocks = (a.n + per_block - 1) / per_block;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * a.col_blocks)), dim3(64 * WAVES), lds, st, a);
+}
+template <bool SWIGLU, bool STREAM>
+static void launch_thin4(Thin4Args a, int64_t tiles, hipStream_t st) {
     constexpr int cols = Thin4<16, SWIGLU, STREAM>::kCols;
     a.split = fp8_thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kSlabBytes, compute_units());
-    const int per_block = waves / a.split * cols;
-    a.col_blocks = (a.n + per_block - 1) / per_block;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * a.col_blocks)), dim3(64 * waves), lds, st, a);
+    if (SWIGLU && a.split == 4)
+        launch_thin4_waves<SWIGLU, STREAM, SWIGLU ? 8 : 4>(a, tiles, st);
+    else
+        launch_thin4_waves<SWIGLU, STREAM, 4>(a, tiles, st);
 }
 
 void launch_fp4_thin(const Fp4Gemm& g, const int32_t* expert_offset, const void* x, const uint8_t* x_scale, int64_t x_rows,

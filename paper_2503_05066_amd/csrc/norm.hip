@@ -2,8 +2,13 @@
 //
 //   h = round(x + residual),  y = round(h / sqrt(mean(h^2) + eps) * weight),  q = the 8- or 4-bit form of y
 //
-// One pass over the data: a row stays in the registers of its waves (rows of more than kNormMostColumns are read twice).  The
-// sum of squares is fp32: a lane adds its values in ascending order, then the lanes, then the waves, always in the same order.
+// One pass over the data: a row stays in the registers of its waves (rows of more than kNormMostColumns are read twice).  Eight
+// squares are added in fp32, those sums in 64 bits for fp32 rows, whose outputs are then as good as rounded once (a row's eights err
+// independently, so their mean does by far less than 2^-24), in 32 bits for bf16 rows (8192 x 4096, 8 bits alone: 21.1 us, with 64
+// bits 23.9): a lane's own in ascending order, then the lanes, then the waves, always in the same order.
+//
+// The bytes bound it where there are many rows: 8192 x 4096 in bf16 with all outputs NORM_US us, a plain copy's rate; few rows take
+// one round trip to memory, the sums and the writes.
 #include <algorithm>
 
 #include "ffn_tile.h"
@@ -56,41 +61,88 @@ __device__ __forceinline__ void write_group_fp8(Eight<BF16> e, int lane, int col
     if (lane == 0) *(uint32_t*)scale = word;
 }
 
-__device__ __forceinline__ float sum_of_wave(float v) {
-    auto add = [&](int other) { v += __int_as_float(other); };
-    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));   // lane ^ 1
-    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));   // lane ^ 2
-    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));  // the other quad of eight lanes
-    add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));  // the other eight of sixteen
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {  // by a DPP control
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+    const int2 w = __builtin_bit_cast(int2, v);
+    return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_update_dpp(0, w.x, CTRL, 0xf, 0xf, false),
+                                                __builtin_amdgcn_update_dpp(0, w.y, CTRL, 0xf, 0xf, false)));
+}
+// v of the lane's row of 16 and of the next one; of either half of the wave
+__device__ __forceinline__ float two_rows(float v) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-    v = __int_as_float((int)a[0]) + __int_as_float((int)a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-    return __int_as_float((int)b[0]) + __int_as_float((int)b[1]);
+    return __int_as_float((int)a[0]) + __int_as_float((int)a[1]);
 }
-
-// 1 / sqrt(mean + eps) from the sum of squares of h * shrink
-__device__ __forceinline__ float inverse_root(float squares, int cols, float eps, float shrink) {
-    return rsqrtf(squares / (float)cols + eps * shrink * shrink) * shrink;
+__device__ __forceinline__ float two_halves(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return __int_as_float((int)a[0]) + __int_as_float((int)a[1]);
 }
-// What a row's values are multiplied by where their squares pass the range of fp32: the least of them that then counts is far above
-// what gets lost.
-constexpr float kNormShrink = 0x1p-80f;
+__device__ __forceinline__ double two_rows(double v) {
+    const int2 w = __builtin_bit_cast(int2, v);
+    const auto x = __builtin_amdgcn_permlane16_swap(w.x, w.x, false, false), y = __builtin_amdgcn_permlane16_swap(w.y, w.y, false, false);
+    return __builtin_bit_cast(double, make_int2((int)x[0], (int)y[0])) + __builtin_bit_cast(double, make_int2((int)x[1], (int)y[1]));
+}
+__device__ __forceinline__ double two_halves(double v) {
+    const int2 w = __builtin_bit_cast(int2, v);
+    const auto x = __builtin_amdgcn_permlane32_swap(w.x, w.x, false, false), y = __builtin_amdgcn_permlane32_swap(w.y, w.y, false, false);
+    return __builtin_bit_cast(double, make_int2((int)x[0], (int)y[0])) + __builtin_bit_cast(double, make_int2((int)x[1], (int)y[1]));
+}
+template <class T>
+__device__ __forceinline__ T sum_of_wave(T v) {
+    v += moved<0xb1>(v);   // lane ^ 1
+    v += moved<0x4e>(v);   // lane ^ 2
+    v += moved<0x141>(v);  // the other quad of eight lanes
+    v += moved<0x140>(v);  // the other eight of sixteen
+    return two_halves(two_rows(v));
+}
 
 // the sum over the waves of a row, in the order of the waves
-template <int WAVES>
-__device__ __forceinline__ float sum_of_row(float v, float* part, int wave) {
+template <int WAVES, class T>
+__device__ __forceinline__ T sum_of_row(T v, double* scratch, int wave) {
     v = sum_of_wave(v);
     if constexpr (WAVES > 1) {
-        __syncthreads();  // the sums before have been read
+        T* part = (T*)scratch;
         if ((threadIdx.x & 63) == 0) part[wave] = v;
         __syncthreads();
-        v = 0.f;
+        v = 0;
         const int first = wave / WAVES * WAVES;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) v += part[first + i];
     }
     return v;
 }
+__device__ __forceinline__ float inverse_root(float squares, int cols, float eps) { return __builtin_amdgcn_rsqf(squares / (float)cols + eps); }
+__device__ __forceinline__ double inverse_root(double squares, int cols, float eps) {
+    const double x = squares * (1.0 / cols) + (double)eps;
+    double r = __builtin_amdgcn_rsq(x);  // to 2^-14 at least; each step squares that
+    if (!(x < __builtin_inf())) return r;
+    r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
+    return __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
+}
+
+template <bool BF16>
+using SumOf = std::conditional_t<BF16, float, double>;
+template <bool BF16>
+__device__ __forceinline__ void add_squares(const Eight<BF16>& h, SumOf<BF16>& squares) {
+    float f[8], s[4];
+    floats(h, f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = __builtin_fmaf(f[k], f[k], f[k + 4] * f[k + 4]);
+    squares += (SumOf<BF16>)((s[0] + s[1]) + (s[2] + s[3]));
+}
+// .. where they leave the range of fp32
+template <bool BF16>
+__device__ __forceinline__ void add_wide_squares(const Eight<BF16>& h, double& squares) {
+    float f[8];
+    floats(h, f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) squares = __builtin_fma((double)f[k], (double)f[k], squares);
+}
+template <class T>
+__device__ __forceinline__ bool beyond(T squares) { return !(squares < (T)__builtin_inff()); }
 
 template <bool BF16>
 __device__ __forceinline__ Eight<BF16> with_residual(const NormArgs& p, const Eight<BF16>& x, const Eight<BF16>& r) {
@@ -103,16 +155,21 @@ __device__ __forceinline__ Eight<BF16> with_residual(const NormArgs& p, const Ei
 
 // a group's outputs
 template <bool BF16>
-__device__ __forceinline__ void write_normed(const NormArgs& p, const Eight<BF16>& h, const Eight<BF16>& w, float inverse, int64_t row,
+__device__ __forceinline__ void write_normed(const NormArgs& p, const Eight<BF16>& h, const Eight<BF16>& w, double inverse, int64_t row,
                                              int group, int lane) {
     const int col = group * kFp4Group + lane * 8;
     float f[8], g[8];
     floats(h, f), floats(w, g);
+    const float hi = (float)inverse, lo = BF16 ? 0.f : (float)(inverse - (double)hi);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] *= inverse;
-    if (p.weight) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= g[i];
+    for (int i = 0; i < 8; ++i) {
+        const float scaled = f[i] * hi;
+        if constexpr (BF16) {  // (two roundings to 24 bits ahead of the one to 8)
+            f[i] = p.weight ? scaled * g[i] : scaled;
+        } else {  // with what the product lost
+            const float rest = __builtin_fmaf(f[i], lo, __builtin_fmaf(f[i], hi, -scaled));
+            f[i] = p.weight ? __builtin_fmaf(scaled, g[i], rest * g[i]) : scaled + rest;
+        }
     }
     Eight<BF16> y = rounded<BF16>(f);
     if (p.y) store(y, (uint8_t*)p.y + row * p.cols * (BF16 ? 2 : 4), col, p.cols);
@@ -137,7 +194,7 @@ __device__ __forceinline__ void write_normed(const NormArgs& p, const Eight<BF16
 template <bool BF16, int WAVES, int GROUPS>
 __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel(const NormArgs p) {
     constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;  // of a block
-    __shared__ float part[WAVES < 4 ? 4 : WAVES];
+    __shared__ double part[WAVES < 4 ? 4 : WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, of_row = wave % WAVES;
     const int64_t row = (int64_t)blockIdx.x * kRows + wave / WAVES;
     const int64_t n_rows = p.row_count ? min(p.n_rows, (int64_t)max(*p.row_count, 0)) : p.n_rows;
@@ -158,28 +215,18 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) w[i].load(p.weight, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
     }
-    float squares = 0.f;
+    SumOf<BF16> squares = 0;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        float f[8];
-        floats(h[i], f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(f[k], f[k], squares);
-    }
+    for (int i = 0; i < GROUPS; ++i) add_squares(h[i], squares);
     squares = sum_of_row<WAVES>(squares, part, wave);
-    float inverse = inverse_root(squares, p.cols, p.eps, 1.0f);
-    const bool large = !(squares < __builtin_inff());
-    if (WAVES == 1 || kRows == 1 ? large : __syncthreads_or(large)) {  // rare
-        float small = 0.f;
+    double inverse = inverse_root(squares, p.cols, p.eps);
+    if (WAVES == 1 || kRows == 1 ? beyond(squares) : __syncthreads_or(beyond(squares))) {  // rare
+        double wide = 0.0;
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) {
-            float f[8];
-            floats(h[i], f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) small = __builtin_fmaf(f[k] * kNormShrink, f[k] * kNormShrink, small);
-        }
-        small = sum_of_row<WAVES>(small, part, wave);
-        if (large) inverse = inverse_root(small, p.cols, p.eps, kNormShrink);
+        for (int i = 0; i < GROUPS; ++i) add_wide_squares(h[i], wide);
+        if (WAVES > 1) __syncthreads();  // the sums before have been read
+        wide = sum_of_row<WAVES>(wide, part, wave);
+        if (beyond(squares)) inverse = inverse_root(wide, p.cols, p.eps);
     }
     if (!valid) return;
 #pragma unroll
@@ -194,7 +241,7 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel
 // Rows that no registers hold: sixteen waves read them twice.  (sum may be x or the residual, so the second time it is read.)
 template <bool BF16>
 __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const NormArgs p) {
-    __shared__ float part[16];
+    __shared__ double part[16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t row = blockIdx.x;
     if (p.row_count && row >= *p.row_count) return;
@@ -214,22 +261,21 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const NormArgs p) 
         }
         return h;
     };
-    auto squares_of = [&](float shrink, bool first) {
-        float squares = 0.f;
-        for (int g = wave; g < groups; g += 16) {
-            const int col = g * kFp4Group + lane * 8;
-            const Eight<BF16> h = load(col, first);
-            if (first && p.sum) store(h, (uint8_t*)p.sum + at, col, p.cols);
-            float f[8];
-            floats(h, f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(f[k] * shrink, f[k] * shrink, squares);
-        }
-        return sum_of_row<16>(squares, part, wave);
-    };
-    const float squares = squares_of(1.0f, true);
-    float inverse = inverse_root(squares, p.cols, p.eps, 1.0f);
-    if (!(squares < __builtin_inff())) inverse = inverse_root(squares_of(kNormShrink, false), p.cols, p.eps, kNormShrink);
+    SumOf<BF16> squares = 0;
+    for (int g = wave; g < groups; g += 16) {
+        const int col = g * kFp4Group + lane * 8;
+        const Eight<BF16> h = load(col, true);
+        if (p.sum) store(h, (uint8_t*)p.sum + at, col, p.cols);
+        add_squares(h, squares);
+    }
+    squares = sum_of_row<16>(squares, part, wave);
+    double inverse = inverse_root(squares, p.cols, p.eps);
+    if (beyond(squares)) {  // rare
+        double wide = 0.0;
+        for (int g = wave; g < groups; g += 16) add_wide_squares(load(g * kFp4Group + lane * 8, false), wide);
+        __syncthreads();  // the sums before have been read
+        inverse = inverse_root(sum_of_row<16>(wide, part, wave), p.cols, p.eps);
+    }
     for (int g = wave; g < groups; g += 16) {
         const int col = g * kFp4Group + lane * 8;
         const Eight<BF16> h = load(col, false);
@@ -246,6 +292,9 @@ static void launch_norm(const NormArgs& p, hipStream_t st) {
         const int rows = waves < 4 ? 4 / waves : 1;
         hipLaunchKernelGGL(kern, dim3((unsigned)((p.n_rows + rows - 1) / rows)), dim3(64 * std::max(waves, 4)), 0, st, p);
     };
+    // Few rows: a group of 512 columns per wave, as many waves as there are.  Many rows in bf16: two (us, 8192 x 4096 with all
+    // outputs: eight waves of one group 54.3, four of two 53.0, two of four 53.9; 37 rows 2.7, 3.2, 4.4; in fp32 99.8, 111, 111 and 3.0, 3.6, 5.3)
+    const bool few = p.n_rows <= 1024 || !BF16;
     if (groups == 1)
         launch(norm_rows_kernel<BF16, 1, 1>, 1);
     else if (groups == 2)
@@ -253,11 +302,11 @@ static void launch_norm(const NormArgs& p, hipStream_t st) {
     else if (groups <= 4)
         launch(norm_rows_kernel<BF16, 4, 1>, 4);
     else if (groups <= 8)
-        launch(norm_rows_kernel<BF16, 4, 2>, 4);
+        few ? launch(norm_rows_kernel<BF16, 8, 1>, 8) : launch(norm_rows_kernel<BF16, 4, 2>, 4);
     else if (groups <= 16)
-        launch(norm_rows_kernel<BF16, 4, 4>, 4);
+        few ? launch(norm_rows_kernel<BF16, 16, 1>, 16) : launch(norm_rows_kernel<BF16, 8, 2>, 8);
     else if (groups <= 32)
-        launch(norm_rows_kernel<BF16, 8, 4>, 8);
+        launch(norm_rows_kernel<BF16, 16, 2>, 16);
     else if (p.cols <= kNormMostColumns)
         launch(norm_rows_kernel<BF16, 16, 4>, 16);
     else
