@@ -7,7 +7,7 @@
 // independently, so their mean does by far less than 2^-24), in 32 bits for bf16 rows (8192 x 4096, 8 bits alone: 21.1 us, with 64
 // bits 23.9): a lane's own in ascending order, then the lanes, then the waves, always in the same order.
 //
-// The bytes bound it where there are many rows: 8192 x 4096 in bf16 with all outputs NORM_US us, a plain copy's rate; few rows take
+// The bytes bound it where there are many rows: 8192 x 4096 in bf16 with a residual, all outputs and 4 bits 46.4 us, 6.15 TB/s; few rows take
 // one round trip to memory, the sums and the writes.
 #include <algorithm>
 
@@ -41,13 +41,13 @@ __device__ __forceinline__ Eight<BF16> rounded(const float (&f)[8]) {
     for (int i = 0; i < (BF16 ? 4 : 8); ++i) e.v[i] = BF16 ? pack_bf16x2(f[(2 * i) % 8], f[(2 * i + 1) % 8]) : __float_as_uint(f[i]);
     return e;
 }
-template <bool BF16>
+template <bool BF16, bool ONCE = false>
 __device__ __forceinline__ void store(const Eight<BF16>& e, void* row, int col, int cols) {
     if constexpr (BF16) {
-        if (col < cols) *(uint4*)((uint16_t*)row + col) = make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]);
+        if (col < cols) store16<ONCE>((uint16_t*)row + col, make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]));
     } else {
-        if (col < cols) *(uint4*)((float*)row + col) = make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]);
-        if (col + 4 < cols) *(uint4*)((float*)row + col + 4) = make_uint4(e.v[4], e.v[5], e.v[6], e.v[7]);
+        if (col < cols) store16<ONCE>((float*)row + col, make_uint4(e.v[0], e.v[1], e.v[2], e.v[3]));
+        if (col + 4 < cols) store16<ONCE>((float*)row + col + 4, make_uint4(e.v[4], e.v[5], e.v[6], e.v[7]));
     }
 }
 
@@ -190,8 +190,10 @@ __device__ __forceinline__ void write_normed(const NormArgs& p, const Eight<BF16
     }
 }
 
-// WAVES waves take a row, GROUPS groups of 512 columns each.
-template <bool BF16, int WAVES, int GROUPS>
+// WAVES waves take a row, GROUPS groups of 512 columns each.  ONCE: x and the residual, which nobody reads after the norm, and the sum,
+// which is read a layer later, are more than the L2s hold and are not kept there (8192 x 4096 with all outputs and the values of its
+// 4-bit rows: 66.2 us, without x and the residual 63.3, without the sum too 59.7, without y 62.5).
+template <bool BF16, int WAVES, int GROUPS, bool ONCE>
 __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel(const NormArgs p) {
     constexpr int kRows = WAVES < 4 ? 4 / WAVES : 1;  // of a block
     __shared__ double part[WAVES < 4 ? 4 : WAVES];
@@ -204,10 +206,10 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel
     const int end = valid ? p.cols : 0;
     Eight<BF16> h[GROUPS], w[GROUPS];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) h[i].load((const uint8_t*)p.x + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
+    for (int i = 0; i < GROUPS; ++i) h[i].template load<ONCE>((const uint8_t*)p.x + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
     if (p.residual) {
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) w[i].load((const uint8_t*)p.residual + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
+        for (int i = 0; i < GROUPS; ++i) w[i].template load<ONCE>((const uint8_t*)p.residual + at, (i * WAVES + of_row) * kFp4Group + lane * 8, end);
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) h[i] = with_residual(p, h[i], w[i]);
     }
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel
     for (int i = 0; i < GROUPS; ++i) {
         const int group = i * WAVES + of_row;
         if (group * kFp4Group >= p.cols) continue;
-        if (p.sum) store(h[i], (uint8_t*)p.sum + at, group * kFp4Group + lane * 8, p.cols);
+        if (p.sum) store<BF16, ONCE>(h[i], (uint8_t*)p.sum + at, group * kFp4Group + lane * 8, p.cols);
         write_normed(p, h[i], w[i], inverse, row, group, lane);
     }
 }
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const NormArgs p) 
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool ONCE>
 static void launch_norm(const NormArgs& p, hipStream_t st) {
     const int groups = fp4_groups(p.cols);
     auto launch = [&](auto kern, int waves) {
@@ -296,19 +298,19 @@ static void launch_norm(const NormArgs& p, hipStream_t st) {
     // outputs: eight waves of one group 54.3, four of two 53.0, two of four 53.9; 37 rows 2.7, 3.2, 4.4; in fp32 99.8, 111, 111 and 3.0, 3.6, 5.3)
     const bool few = p.n_rows <= 1024 || !BF16;
     if (groups == 1)
-        launch(norm_rows_kernel<BF16, 1, 1>, 1);
+        launch(norm_rows_kernel<BF16, 1, 1, ONCE>, 1);
     else if (groups == 2)
-        launch(norm_rows_kernel<BF16, 2, 1>, 2);
+        launch(norm_rows_kernel<BF16, 2, 1, ONCE>, 2);
     else if (groups <= 4)
-        launch(norm_rows_kernel<BF16, 4, 1>, 4);
+        launch(norm_rows_kernel<BF16, 4, 1, ONCE>, 4);
     else if (groups <= 8)
-        few ? launch(norm_rows_kernel<BF16, 8, 1>, 8) : launch(norm_rows_kernel<BF16, 4, 2>, 4);
+        few ? launch(norm_rows_kernel<BF16, 8, 1, ONCE>, 8) : launch(norm_rows_kernel<BF16, 4, 2, ONCE>, 4);
     else if (groups <= 16)
-        few ? launch(norm_rows_kernel<BF16, 16, 1>, 16) : launch(norm_rows_kernel<BF16, 8, 2>, 8);
+        few ? launch(norm_rows_kernel<BF16, 16, 1, ONCE>, 16) : launch(norm_rows_kernel<BF16, 8, 2, ONCE>, 8);
     else if (groups <= 32)
-        launch(norm_rows_kernel<BF16, 16, 2>, 16);
+        launch(norm_rows_kernel<BF16, 16, 2, ONCE>, 16);
     else if (p.cols <= kNormMostColumns)
-        launch(norm_rows_kernel<BF16, 16, 4>, 16);
+        launch(norm_rows_kernel<BF16, 16, 4, ONCE>, 16);
     else
         launch(norm_long_rows_kernel<BF16>, 16);
 }
@@ -318,10 +320,10 @@ hipError_t launch_norm_rows(const moe_norm_t& norm, const void* x, const void* r
     NormArgs p;
     p.x = x, p.residual = residual, p.weight = weight, p.row_count = row_count, p.sum = sum, p.y = y;
     p.q = (uint8_t*)q, p.scale = scale, p.n_rows = norm.n_rows, p.cols = norm.cols, p.bits = norm.bits, p.eps = norm.eps;
-    if (norm.dtype == MOE_DTYPE_BF16)
-        launch_norm<true>(p, st);
-    else
-        launch_norm<false>(p, st);
+    // (of fp32 rows a lane's two requests share lines with its neighbours': 99.5 us with the lines kept, 123 without)
+    const bool bf16 = norm.dtype == MOE_DTYPE_BF16, once = (double)p.n_rows * p.cols * 2 > kL2Bytes;
+    auto launch = bf16 ? (once ? launch_norm<true, true> : launch_norm<true, false>) : launch_norm<false, false>;
+    launch(p, st);
     return hipGetLastError();
 }
 

@@ -16,20 +16,44 @@ struct Divisor {
     __device__ __forceinline__ uint32_t divide(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> (31 + s)); }
 };
 
+constexpr double kL2Bytes = 32 << 20;  // of the eight XCDs together
+
+// ONCE: the line is not kept in the caches.
+template <bool ONCE>
+__device__ __forceinline__ uint4 load16(const void* p) {
+    if constexpr (ONCE) {
+        typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+        const u32x4 v = __builtin_nontemporal_load((const u32x4*)p);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+        return *(const uint4*)p;
+    }
+}
+template <bool ONCE>
+__device__ __forceinline__ void store16(void* p, const uint4& v) {
+    if constexpr (ONCE) {
+        typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+        __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4*)p);
+    } else {
+        *(uint4*)p = v;
+    }
+}
+
 // Eight values of a lane, of a row that begins at x and has `cols` of them, from column col; zeros behind the row's end.
 template <bool BF16>
 struct Eight {
     uint32_t v[BF16 ? 4 : 8];
+    template <bool ONCE = false>
     __device__ __forceinline__ void load(const void* row, int col, int cols) {
         if (BF16) {
             uint4 p = make_uint4(0, 0, 0, 0);
-            if (col < cols) p = *(const uint4*)((const uint16_t*)row + col);
+            if (col < cols) p = load16<ONCE>((const uint16_t*)row + col);
             v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint4 p = make_uint4(0, 0, 0, 0);
-                if (col + 4 * h < cols) p = *(const uint4*)((const float*)row + col + 4 * h);
+                if (col + 4 * h < cols) p = load16<ONCE>((const float*)row + col + 4 * h);
                 v[(4 * h) % (BF16 ? 4 : 8)] = p.x, v[(4 * h + 1) % (BF16 ? 4 : 8)] = p.y;
                 v[(4 * h + 2) % (BF16 ? 4 : 8)] = p.z, v[(4 * h + 3) % (BF16 ? 4 : 8)] = p.w;
             }
