@@ -531,7 +531,7 @@ void launch_fp4_shape(Fp4Args p, hipStream_t st) {
         (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLdsBytes);
     });
     const int nb = p.n_pad / S::kNCols;
-    p.tile_shift = fp8_tile_shift(p.max_rows, p.experts, nb, compute_units());
+    p.tile_shift = fp4_tile_shift(p.max_rows, nb, compute_units());
     // a block per compute unit, the same number on every XCD (which of them get items is known on the device only)
     const int grid = 8 * std::max(1, compute_units() / 8);
     p.col_group = nb % 4 == 0 ? 4 : (nb % 3 == 0 ? 3 : (nb % 2 == 0 ? 2 : 1));

@@ -28,21 +28,58 @@ inline Fp4Gemm fp4_gemm(int experts, int64_t max_rows, int k, int n) {
     return Fp4Gemm{experts, max_rows, k, fp4_pitch(k), fp4_scale_pitch(k), n, fp8_pitch(n)};
 }
 
-// Which kernels an FFN or a product takes: those for few rows (fp4_thin.hip) or on high row tiles.
+// Which kernels an FFN or a product takes: those for few rows (fp4_thin.hip), which make passes of 32 rows over an expert's weights, or those
+// on high row tiles (fp4.hip).  Few rows against tiles, rows dealt evenly, us.  FFN: one token of 64 x 2048 x 1024 11.6 and 20.2, 16 (2
+// rows an expert) 41.4 and 50.3, 128 (16) 41.6 and 51.3; 64 x 2048 x 1408, 8 rows 59 and 69, 16 63.5 and 70, 24 69.8 and 71; 32 x 4096 x 1408,
+// 8 62.6 and 71.4, 16 67 and 73, 24 74.4 and 74.2; 8 x 4096 x 4096, 16 39.8 and 45.4, 32 42.8 and 46.3; with more weights than the memory-side
+// cache holds 16 x 2048 x 8192, 8 80 and 84, 16 87 and 85; 64 x 1024 x 4096, 8 88 and 90, 16 93 and 92; 8 x 4096 x 14336, 4 127 and 132, 8 132 and
+// 132, 16 148 and 135; with few weights 8 x 2048 x 1024, 16 12.3 and 20.8, 1 x 4096 x 2048, 32 14.7 and 25.2, 64 23.2 and 27.7.  Products:
+// 64 x 2048 x 1024, 2 13.8 and 15.6, 16 14.3 and 15.9; 8 of 14336 columns by 4096, 4 37.1 and 38.0, 16 40.0 and 38.8; 1 of 2056 x 5640, 32 5.1 and 8.9, 64 8.2
+// and 9.7, 96 11.1 and 9.8.
+// How the rows lie is known on the device only, and the passes over a long expert run one after the other in its own blocks: the most rows
+// that an expert may have are four passes (see fp8_forms.h).
+constexpr int kFp4PassRows = 32;
 inline bool fp4_ffn_is_few_rows(const moe_desc_t& d, const Sizes& s) {
-    const bool few = fp8_few_weights(3.0 * d.n_experts * fp4_pitch(d.d_model) * fp8_pitch(d.d_hidden));
+    const double bytes = 3.0 * d.n_experts * fp4_pitch(d.d_model) * fp8_pitch(d.d_hidden);
     const int64_t most = std::min<int64_t>((int64_t)s.n_blocks * s.cap, d.n_tokens);  // rows of an expert
-    return most <= (few ? 32 : 16) || (most <= kFp8MostPasses * 16 && s.max_rows <= (few ? 16ll : 4ll) * d.n_experts);
+    const int64_t rows = fp8_few_weights(bytes) ? 32 : (fp8_weights_stream(bytes) ? 8 : 16);
+    return most <= kFp8MostPasses * kFp4PassRows && s.max_rows <= rows * d.n_experts;
 }
 inline bool fp4_gemm_is_few_rows(const Fp4Gemm& g) {
     const bool few = fp8_few_weights((double)g.experts * g.pitch * g.n_pad);
-    return g.max_rows <= (few ? 64 : 32) || (g.max_rows <= kFp8MostPasses * 32 && g.max_rows <= (few ? 32ll : 8ll) * g.experts);
+    return g.max_rows <= (few ? 64 : 32) || (g.max_rows <= kFp8MostPasses * kFp4PassRows && g.max_rows <= (few ? 32ll : 8ll) * g.experts);
 }
 
-// Which width a product on high tiles takes, 256 or 128 columns.
+// How many waves share a weight row.  Eight waves fill a compute unit; whole rows keep a wave's ring full for longer, shorter parts end sooner and
+// more alike.  At 4, 2, 1 (256 compute units): products of one row of 8 x 2048 x 1024 (256 waves) 4.2, 4.9, 6.3 us, of 64 (2048) 18.1, 15.4, 14.1; 2 rows
+// each of 8 of 14336 columns by 4096 (1024, 56 slabs) 36.8, 38.8, 37.9; 4 of 8 of 4096 by 14336 (3584, 16 slabs) 42.8, 37.8, 38.2; the FFN of 16 tokens on
+// 8 x 4096 x 14336 (7168, 16 slabs, and 1024) 160, 128, 132, on 16 x 4096 x 7168 (7168, 16 and 2048, 28) 2 rows each 123, 129 at 2, 1; on 32 x 4096 x 1408
+// (2816, 16 and 4096, 6), whose weights the memory-side cache holds, 62.4, 59.9; 8 x 4096 x 4096 (2048, 16 and 1024, 16) 39.9, 39.4.
+inline int fp4_thin_split(int64_t waves, int slabs, bool stream, int cus) {
+    if (waves <= 2 * cus || (waves <= 4 * cus && slabs >= 32)) return 4;
+    return waves <= 4 * cus || (stream && slabs >= 16) ? 2 : 1;
+}
+
+// Rows of a full row tile (1 << the result; columns: column blocks of the product): lower tiles as long as the items of full ones fit one
+// round of the compute units (items of an expert's last rows are short).  Tiles of 64, 128, 256 rows, us, on 256 compute units: one expert, 203
+// rows of 2056 x 5640 (narrow) 10.3, 13.1, 15.0, 512 17.0, 14.0, 17.0, 1024 23.4, 23.1, 18.9; 2048 of 4096 x 4096 (wide) 32.9, 27.3, 42.9; 8 x 256 of 14336
+// by 4096 (wide) 109, 76, 94; 8 x 300 of 4096 x 4096 47.8, 41.9, 40.0; FFN of 512 tokens top-2 on 8 x 2048 x 1024 26.2, 34.6, 34.7, 1024 33.6, 36.9,
+// 48.1, 2048 51.5, 45.8, 50.1; 1500 on 8 x 4096 x 4096 103, 93, 74.
+inline int fp4_tile_shift(int64_t max_rows, int columns, int cus) {
+    int shift = 8;
+    while (shift > 6 && columns * (max_rows >> (shift - 1)) <= cus) --shift;
+    return shift;
+}
+
+// Which width a product on high tiles takes, 256 or 128 columns: narrower tiles where the wide ones, of 128 rows at least and with the
+// rows dealt evenly, would leave a quarter of the compute units without an item.  Wide and narrow, us: 64 x 32 rows of 2048 x 1024 16.2, 17.4;
+// 8 x 16 of 14336 by 4096 43.2, 38.8, 8 x 128 55.3, 53.3, 8 x 256 76.0, 77.8; 2048 of 4096 x 4096 27.3, 29.2; 64 of 4096 x 14336 17.0, 12.8.
 inline bool fp4_tiles_are_wide(const Fp4Gemm& g, int cus) {
-    const int64_t tiles = g.max_rows / kFfnTileM + std::min<int64_t>(g.max_rows, g.experts);
-    return g.n_pad % 256 == 0 && 4 * tiles * (g.n_pad / 256) > 3 * cus;
+    if (g.n_pad % 256 != 0 || g.max_rows == 0) return false;
+    const int columns = g.n_pad / 256;
+    const int64_t height = (int64_t)1 << std::max(7, fp4_tile_shift(g.max_rows, columns, cus));
+    const int64_t active = std::min<int64_t>(g.max_rows, g.experts), rows = (g.max_rows + active - 1) / active;
+    return 4 * active * ((rows + height - 1) / height) * columns > 3 * cus;
 }
 
 }  // namespace capmoe

@@ -315,7 +315,7 @@ static void launch_thin4_waves(Thin4Args a, int64_t tiles, hipStream_t st) {
 template <bool SWIGLU, bool STREAM>
 static void launch_thin4(Thin4Args a, int64_t tiles, hipStream_t st) {
     constexpr int cols = Thin4<16, SWIGLU, STREAM>::kCols;
-    a.split = fp8_thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kSlabBytes, compute_units());
+    a.split = fp4_thin_split(tiles * ((a.n + cols - 1) / cols), a.pitch / kSlabBytes, STREAM, compute_units());
     if (SWIGLU && a.split == 4)
         launch_thin4_waves<SWIGLU, STREAM, SWIGLU ? 8 : 4>(a, tiles, st);
     else
