@@ -609,3 +609,108 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a.y, b.y) and torch.equal(a.expert_offset, b.expert_offset)
+
+
+# ---------------------------------------------------------------------------------------------
+# Cases by the form that the call takes (test_fp4_forms.py holds the forms against the rules): few rows with 4, 2 or 1 waves to a weight
+# row, or column width x row tile.  (rows per expert, columns of x, columns of y, form)
+# ---------------------------------------------------------------------------------------------
+PRODUCT_FORMS = [
+    ([128], 520, 4104, "128x64"), ([0, 60, 0, 4], 2568, 264, "few/4"), ([0, 120, 0, 8], 264, 392, "few/4"),
+    ([1, 0] * 8 + [70, 0, 22], 136, 1032, "few/2"), ([3, 0, 1, 40] + [1] * 16 + [33], 1032, 1000, "few/2"),
+    ([0, 1] * 20 + [65, 0, 23], 520, 1032, "few/1"), ([100] + [0, 1] * 14, 2056, 2056, "few/1"),
+    ([600, 1, 700, 0, 333, 200, 9, 3, 64, 128, 12, 288], 520, 4352, "256x256"), ([300, 1, 400, 0, 33, 200, 9, 3, 64, 128, 12, 88], 1032, 4352, "256x128"),
+    ([300, 1, 0, 20], 1032, 136, "128x64"), ([700, 1, 400], 264, 2048, "128x128"), ([900, 33, 0, 400], 776, 3712, "128x256"),
+    ([40, 1, 0, 20, 33, 0, 9, 3, 2, 1, 12, 8], 392, 4352, "256x64")]
+
+
+@pytest.mark.parametrize("counts,k,n,form", PRODUCT_FORMS)
+def test_product_of_every_form(counts, k, n, form):
+    p = Product(counts, k, n)
+    p.check(p.run())
+    p = Product(counts, k, n, src=31)
+    p.check(p.run())
+
+
+def random_rows(n, k, seed):
+    """4-bit rows on the device: random codes, scale bytes 126 to 128."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, s = capmoe.fp4_row_buffers(n, k)
+    assert k % 512 == 0 or k % 512 == 256
+    q.random_(0, 256, generator=g)
+    s.random_(126, 129, generator=g)
+    if k % 512:
+        s.view(n, -1, 4, 4)[:, -1, :, 2:] = 0
+    return q, s
+
+
+def device_value(q, s):
+    """4-bit rows in 64 bits on the device."""
+    levels = torch.tensor(ref.E2M1, device="cuda")
+    code = torch.stack([q & 15, q >> 4], dim=2).flatten(1)
+    byte = s.view(len(s), -1, 4, 4).transpose(2, 3).reshape(s.shape)[:, : code.shape[1] // 32]
+    return levels[code.long()] * torch.exp2(byte.double() - 127).repeat_interleave(32, 1)
+
+
+# every height in steps of 32 rows, and experts with two tiles (whose weights are kept)
+HEIGHTS = [256, 225, 200, 161, 129, 100, 65, 40, 31, 300, 0, 1]
+STREAMED_PRODUCTS = [(HEIGHTS, 14336, 6144, "256x256 stream"), (HEIGHTS, 14080, 6144, "256x256 stream"), (HEIGHTS, 14080, 4352, "256x128 stream"), (HEIGHTS, 15616, 3712, "128x256 stream"),
+                     ([5, 0, 1, 16, 9, 0, 2, 30, 0, 1, 0, 0], 14336, 4096, "few/2 stream"), ([1, 0, 1, 0, 0, 2, 0, 0, 1, 0, 0, 0], 14080, 4096, "few/4 stream"),
+                     ([3, 0, 1, 0, 33, 2, 0, 0, 1, 0, 0, 0], 3328, 20480, "few/1 stream"), ([3, 0, 1, 0, 33, 2, 0, 0, 1, 0, 0, 0], 7936, 8192, "few/2 stream")]
+
+
+@pytest.mark.parametrize("counts,k,n,form", STREAMED_PRODUCTS)
+def test_streamed_product_of_every_form(counts, k, n, form):
+    # odd and even numbers of slabs: walks over k that begin in the middle wrap around
+    e, rows = len(counts), sum(counts)
+    pitch, scale_pitch = capmoe.moe_fp4_query(k)
+    w, ws = random_rows(e * n, k, 1)
+    x, xs = random_rows(rows, k, 2)
+    offset = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    y = torch.full((rows, n), 7.0, dtype=BF16, device="cuda")
+    capmoe.moe_grouped_gemm_fp4(capmoe.make_gemm(rows, k, n, e), x, xs, None, on(offset), w.view(e, n, pitch), ws.view(e, n, scale_pitch), y)
+    xv = device_value(x, xs)
+    for i in range(e):
+        if counts[i]:
+            want = xv[offset[i]:offset[i + 1]] @ device_value(w[i * n:(i + 1) * n], ws[i * n:(i + 1) * n]).T
+            assert torch.equal(y[offset[i]:offset[i + 1]].double(), on(ref.to_bf16(plain(want)))), i
+
+
+# tokens, top-k, rows per expert, d, h, forms of the two products
+STREAMED_FFNS = [(600, 4, HEIGHTS, 4352, 4608, "128x256 256x256 stream"), (600, 4, HEIGHTS, 4224, 4480, "128x256 128x256 stream"),
+                 (24, 2, [16, 3, 0, 1, 24, 0, 2, 0, 0, 1, 0, 0], 4352, 4480, "few/2 few/2 stream"), (2, 2, [0, 2, 0, 0, 0, 1, 0, 0, 0, 0, 1, 0], 4096, 4608, "few/2 few/4 stream"),
+                 (1, 2, [0, 0, 0, 1, 0, 0, 0, 0, 0, 0, 0, 1], 5120, 4096, "few/4 few/4 stream"), (90, 1, [40, 0, 0, 33, 0, 0, 9, 0, 0, 0, 0, 8], 3328, 6144, "few/1 few/2 stream")]
+
+
+@pytest.mark.parametrize("tokens,k,counts,d,h,forms", STREAMED_FFNS)
+def test_streamed_ffn_of_every_form(tokens, k, counts, d, h, forms):
+    e, rows = len(counts), sum(counts)
+    desc = capmoe.make_desc(tokens, d, e, k, h, mode=capmoe.MODE_NONE)
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    parts = []
+    for n, c in ((h, d), (h, d), (d, h)):
+        q, s = capmoe.fp4_weight_buffers(e, n, c)
+        for i in range(e):
+            w = torch.randn((1, n, c // 128, 128), generator=g, device="cuda") * c ** -0.5
+            w *= torch.exp2(torch.randint(-2, 3, (1, n, c // 128, 1), generator=g, device="cuda").float())
+            capmoe.moe_quantize_weights_fp4(w.view(1, n, c), q[i:i + 1], s[i:i + 1])
+        parts.append((q, s))
+    experts = capmoe.Fp4Experts(*[t for p in parts for t in p])
+    x = on(rng(31, tokens).standard_normal((tokens, d)), BF16)
+    offset, token = plan_of(rng(32, tokens), tokens, counts)
+    padded = np.zeros(max(tokens * k, rows), np.int32)
+    padded[:rows] = token
+    yp = torch.full((tokens * k, d), 7.0, dtype=BF16, device="cuda")
+    ws = torch.empty(capmoe.moe_query_fp4(desc), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xFF)
+    capmoe.moe_dispatch_ffn_fp4(desc, x, None, on(offset), on(padded), experts, yp, ws)
+    assert torch.all(yp[rows:] == 7.0)
+    xv = on(ref.value(*ref.quantize(plain(x)))[token])
+    want = np.zeros((rows, d))
+    for i in np.flatnonzero(counts):
+        gate, up, down = (device_value(q[i], s[i]) for q, s in parts)
+        a = xv[offset[i]:offset[i + 1]]
+        gv, uv = plain(a @ gate.T), plain(a @ up.T)
+        hidden = ref.value(*ref.quantize(ref.to_bf16(gv / (1 + np.exp(-gv)) * uv)[:, :h]))
+        want[offset[i]:offset[i + 1]] = plain(on(hidden) @ down.T)[:, :d]
+    assert_close(plain(yp[:rows]), want, h)
