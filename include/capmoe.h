@@ -417,8 +417,8 @@ int moe_query_fp4(const moe_desc_t* desc, size_t* workspace_bytes);
  * The rows that the experts read are x in 4 bits: with x_scale == NULL, x is bf16 and is quantised on the way; otherwise x holds
  * 4-bit rows, as moe_norm_rows or moe_quantize_rows_fp4 leave them, and x_scale their scales.  The layer's router always reads bf16,
  * x; xq and xq_scale, both or neither, are the same rows in 4 bits.  The hidden activation is rounded to bf16 once, then to 4 bits.
- * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp4 and moe_layer_forward_fp4: N * d < 2^31; all three:
- * P_max < 2^31 and max(P_max, N) * ceil(max(d, h) / 512) < 2^31; else MOE_ERR_UNSUPPORTED.  Where no row can survive (P_max = 0)
+ * Rows at or behind expert_offset[E] of yp stay untouched.  moe_dispatch_ffn_fp4 and moe_layer_forward_fp4: N * d < 2^31 and
+ * N * pitch(d) < 2^32 - 15; all three: P_max < 2^31 and max(P_max, N) * ceil(max(d, h) / 512) < 2^31; else MOE_ERR_UNSUPPORTED.  Where no row can survive (P_max = 0)
  * nothing is enqueued for the FFN, and x, xp, row_token and yp may be null.
  * Where the quantising of x is a launch of its own, a profile table counts it as MOE_KERNEL_DISPATCH.
  */

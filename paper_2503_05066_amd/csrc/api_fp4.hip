@@ -50,7 +50,10 @@ static int validate_fp4(const moe_desc_t* d) {
 }
 
 // The first product addresses all of x, as bf16 or as 4-bit rows, through one window of 4 GiB.
-static bool too_large_to_gather(const moe_desc_t* d) { return (uint64_t)d->n_tokens * (uint64_t)d->d_model >= (1ull << 31); }
+static bool too_large_to_gather(const moe_desc_t* d) {
+    return (uint64_t)d->n_tokens * (uint64_t)d->d_model >= (1ull << 31) ||
+           (uint64_t)d->n_tokens * (uint64_t)fp4_pitch(d->d_model) > kBeyond;
+}
 
 static int validate_experts4(const moe_fp4_experts_t* w) {
     if (!w || !w->gate || !w->gate_scale || !w->up || !w->up_scale || !w->down || !w->down_scale) return MOE_ERR_INVALID_ARG;

@@ -201,6 +201,10 @@ def test_ffn_refusals():
         assert call(desc=_desc(gamma=0.0), x=None, token=None, yp=None) == OK  # no row can survive
     big = _desc(n_tokens=1 << 18, d_model=1 << 13)
     assert lib.moe_dispatch_ffn_fp4(ctypes.byref(big), P, None, P, P, ctypes.byref(_experts()), P, P, 1 << 50, None) == UNSUPPORTED
+    # narrow rows of many tokens: 2^25 of 128 bytes pass the window that they are gathered through
+    narrow = _desc(n_tokens=1 << 25, d_model=8, n_experts=8, top_k=1, d_hidden=8)
+    for scale in (None, P):
+        assert lib.moe_dispatch_ffn_fp4(ctypes.byref(narrow), P, scale, P, P, ctypes.byref(_experts()), P, P, 1 << 50, None) == UNSUPPORTED
 
 
 def test_layer_refusals():
@@ -222,6 +226,7 @@ def test_layer_refusals():
         assert call(**{a: P + 8}) == INVALID, a
     assert call(xq=P + 8, xs=P) == INVALID and call(xq=P, xs=P + 4) == INVALID
     assert call(size=64) == SMALL and call(desc=_desc(dtype=capmoe.DTYPE_F32)) == UNSUPPORTED
+    assert call(desc=_desc(n_tokens=1 << 25, d_model=8, n_experts=8, top_k=1, d_hidden=8), size=1 << 50) == UNSUPPORTED
 
 
 def test_binding_refuses_tensors_that_do_not_fit():
