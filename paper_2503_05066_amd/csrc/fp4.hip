@@ -55,7 +55,8 @@ struct Shape4 : Shape<BN_, SWIGLU_> {
     // Slabs at the end of an item that run without some of the requests.  The scales of slab kt + 4 or what lies beside them are
     // requested in slab kt, so these slabs request none.
     static constexpr int kTail = 3;
-    static_assert(units(8) >= 4 && units(1) == kTail && units(2) == kTail, "ring");
+    // (the bounds that the scales' requests ask for, see MatrixLoop4)
+    static_assert(units(8) >= 4 && units(3) <= 6 && units(1) == kTail && units(2) == kTail, "ring");
     // which half of the activations the first slab of an item begins with: such that the tail always begins with the first
     static __host__ __device__ constexpr int parity(int slabs) {
         const int left = slabs - kTail;
@@ -192,11 +193,11 @@ struct Fills4 {
 };
 
 // K loop of a wave.  LIVE = number of 16-row activation sub-tiles per wave that are fetched and multiplied.  How a slab is walked in
-// parts, read and requested stands at MatrixLoop8 (fp8.hip).  The scales add:
-//   request i (see one_scale) is made in slab i - 4, ahead of the unit that is requested there first: number 2 (i - 4) + NU of the half slabs,
-//   or i - 4 + NU of the slabs, so it has landed when that unit has, and with it group i / 2 = 2 (i / 4) .. ahead of unit 2 i or i,
-//   behind whose barrier the waves read their bytes of the group's first slab;
-//   its slot (group mod 3) was read for the last time in the slab before.
+// parts, read and requested stands at MatrixLoop8 (fp8.hip).  The scales add one request per wave and slab: slab kt makes request
+// i = kt + 4 (see one_scale) ahead of its first unit's, which is unit 2 kt + NU of half slabs, or kt + NU of slabs.  So
+//   - a group's two requests (i = 2 g, 2 g + 1) have landed when unit 4 g of half slabs, or 2 g of slabs, has: the first of the group's
+//     first slab, behind whose barrier the waves begin to read the group (2 (2 g - 3) + NU <= 4 g and 2 g - 3 + NU <= 2 g hold for the rings);
+//   - the slot (g mod 3) was read for the last time in slab 2 g - 5, and the first request for it is made behind a barrier of slab 2 g - 4.
 // The waits count the requests that are younger than the unit they wait for, and with them those for scales ahead of younger units.
 template <class S, bool ONCE>
 struct MatrixLoop4 {

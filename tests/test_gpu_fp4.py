@@ -93,15 +93,51 @@ def test_eight_bit_rows_back_to_values(rows, cols, dtype):
     assert np.array_equal(plain(y), torch.from_numpy(want).to(dtype).double().numpy(), equal_nan=True)
 
 
-def test_rows_narrower_than_eight_of_fp32():
-    x = on(rng(4).standard_normal((5, 4)), F32)
-    q, s = capmoe.fp4_row_buffers(5, 4)
+@pytest.mark.parametrize("cols", [4, 12, 36, 516, 1020])
+def test_rows_of_fp32_that_end_in_the_middle_of_eight(cols):
+    x = on(rng(4, cols).standard_normal((5, cols)), F32)
+    q, s = capmoe.fp4_row_buffers(5, cols)
     capmoe.moe_quantize_rows_fp4(x, None, None, q, s)
     want_q, want_s = ref.quantize(plain(x))
     assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(s.cpu().numpy(), want_s)
-    y = torch.full((5, 4), 7.0, device="cuda")
+    y = torch.full((5, cols), 7.0, device="cuda")
     capmoe.moe_dequantize_rows(4, q, s, y)
-    assert np.array_equal(plain(y), ref.value(want_q, want_s)[:, :4])
+    assert np.array_equal(plain(y), ref.value(want_q, want_s)[:, :cols])
+    q8, s8 = capmoe.fp8_row_buffers(5, cols)
+    capmoe.moe_quantize_rows(x, None, None, q8, s8)
+    y.fill_(7.0)
+    capmoe.moe_dequantize_rows(8, q8, s8, y)
+    assert np.array_equal(plain(y), ref8.rows_value(q8.cpu().numpy(), s8.cpu().numpy())[:, :cols])
+
+
+def test_rows_that_a_plan_names_more_than_once_and_out_of_order():
+    p = Product([5, 0, 70], 520, 264, src=9)
+    p.token[:] = np.array([8, 8, 0, 3, 3] + [8 - i % 9 for i in range(70)], np.int32)
+    p.check(p.run())
+
+
+def test_product_of_rows_beyond_31_bit_offsets():
+    # 3 GiB of rows, fetched through a plan and in their order
+    k, n, src = 12288, 128, 1 << 19
+    x, xs = random_rows(src, k, 3)
+    w, ws = random_rows(n, k, 4)
+    pitch, scale_pitch = capmoe.moe_fp4_query(k)
+    token = np.array([0, src - 1, src // 2, 5, src - 2, (1 << 31) // pitch, (1 << 31) // pitch + 1] * 20, np.int32)
+    wv = device_value(w, ws)
+    for rows, room in ((7, 7), (140, 140), (140, 20000)):
+        offset = on(np.array([0, rows], np.int32))
+        numbers = on(np.concatenate([token[:rows], np.zeros(room - rows, np.int32)]))
+        y = torch.full((room, n), 7.0, dtype=BF16, device="cuda")
+        capmoe.moe_grouped_gemm_fp4(capmoe.make_gemm(room, k, n, 1, src_rows=src), x, xs, numbers, offset, w.view(1, n, pitch),
+                                    ws.view(1, n, scale_pitch), y)
+        at = on(token[:rows]).long()
+        assert torch.equal(y[:rows].double(), on(ref.to_bf16(plain(device_value(x[at], xs[at]) @ wv.T))))
+    offset = on(np.array([0, 10, src], np.int32))
+    y = torch.full((src, n), 7.0, dtype=BF16, device="cuda")
+    capmoe.moe_grouped_gemm_fp4(capmoe.make_gemm(src, k, n, 2), x, xs, None, offset, torch.stack([w, w]).view(2, n, pitch),
+                                torch.stack([ws, ws]).view(2, n, scale_pitch), y)
+    for part in (slice(0, 300), slice(src // 2, src // 2 + 300), slice(src - 300, src)):
+        assert torch.equal(y[part].double(), on(ref.to_bf16(plain(device_value(x[part], xs[part]) @ wv.T))))
 
 
 @pytest.mark.parametrize("count", [-3, 0, 1, 40, 64, 1000])

@@ -101,6 +101,36 @@ def test_narrow_rows_of_fp32():
     check(x, None, None, norm.eps, None, y, q, s, 8)
 
 
+@pytest.mark.parametrize("cols", [12, 36, 516, 1020, 4100, 33004])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_fp32_rows_that_end_in_the_middle_of_eight(cols, bits):
+    x, r, w = values(30, 6, cols, F32), values(31, 6, cols, F32), values(32, 1, cols, F32)[0]
+    x[2, cols - 1] = float("nan")  # a row that is no number ends in zeros all the same
+    h, y = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    q, s = buffers(6, cols, bits)
+    norm = capmoe.make_norm(6, cols, 1e-6, capmoe.DTYPE_F32, bits)
+    capmoe.moe_norm_rows(norm, x, r, w, None, h, y, q, s)
+    check(x, r, w, norm.eps, h, y, q, s, bits)
+
+
+def test_rows_beyond_32_bit_offsets():
+    rows, cols = 600000, 4096  # 4.9 GB each
+    x = torch.zeros((rows, cols), dtype=BF16, device="cuda")
+    last = values(33, 5, cols, BF16)
+    x[-5:], x[:5] = last, last
+    y, (q, s) = torch.full_like(x, 7.0), buffers(rows, cols, 4)
+    capmoe.moe_norm_rows(capmoe.make_norm(rows, cols, bits=4), x, None, None, None, None, y, q, s)
+    norm = capmoe.make_norm(5, cols, 1e-6, bits=4)
+    check(last, None, None, norm.eps, None, y[-5:], q[-5:], s[-5:], 4)
+    assert torch.equal(y[:5], y[-5:]) and torch.equal(q[:5], q[-5:]) and not y[5:-5].any() and not q[5:-5].any()
+    x[:] = 0
+    capmoe.moe_dequantize_rows(4, q, s, x)
+    assert np.array_equal(f64(x[-5:]), ref4.value(q[-5:].cpu().numpy(), s[-5:].cpu().numpy())) and torch.equal(x[:5], x[-5:])
+    q2, s2 = buffers(rows, cols, 4)
+    capmoe.moe_quantize_rows_fp4(y, None, None, q2, s2)
+    assert torch.equal(q, q2) and torch.equal(s, s2)
+
+
 @pytest.mark.parametrize("cols", [264, 1024, 4096, 40000])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_outputs_in_place_of_inputs(cols, dtype):
