@@ -2,10 +2,10 @@
 //
 //   h = round(x + residual),  y = round(h / sqrt(mean(h^2) + eps) * weight),  q = the 8- or 4-bit form of y
 //
-// One pass over the data: a row stays in the registers of its waves (rows of more than kNormMostColumns are read twice).  Eight
-// squares are added in fp32, those sums in 64 bits for fp32 rows, whose outputs are then as good as rounded once (a row's eights err
-// independently, so their mean does by far less than 2^-24), in 32 bits for bf16 rows (8192 x 4096, 8 bits alone: 21.1 us, with 64
-// bits 23.9): a lane's own in ascending order, then the lanes, then the waves, always in the same order.
+// One pass over the data: a row stays in the registers of its waves (rows of more than kNormMostColumns are read twice).  The
+// squares of fp32 rows are added in 64 bits, which costs nothing beside the reads, and their outputs are as good as rounded once; those of
+// bf16 rows in 32 bits (with the sums of eights in 64, 8192 x 4096 to 8 bits alone take 23.9 us instead of 21.1), and once more in 64 where they leave
+// the range of fp32.  A lane's own come first, then the lanes, then the waves, always in the same order.
 //
 // The bytes bound it where there are many rows: 8192 x 4096 in bf16 with a residual, all outputs and 4 bits 46.4 us, 6.15 TB/s; few rows take
 // one round trip to memory, the sums and the writes.
@@ -126,20 +126,24 @@ __device__ __forceinline__ double inverse_root(double squares, int cols, float e
 template <bool BF16>
 using SumOf = std::conditional_t<BF16, float, double>;
 template <bool BF16>
-__device__ __forceinline__ void add_squares(const Eight<BF16>& h, SumOf<BF16>& squares) {
-    float f[8], s[4];
-    floats(h, f);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] = __builtin_fmaf(f[k], f[k], f[k + 4] * f[k + 4]);
-    squares += (SumOf<BF16>)((s[0] + s[1]) + (s[2] + s[3]));
-}
-// .. where they leave the range of fp32
-template <bool BF16>
 __device__ __forceinline__ void add_wide_squares(const Eight<BF16>& h, double& squares) {
     float f[8];
     floats(h, f);
 #pragma unroll
     for (int k = 0; k < 8; ++k) squares = __builtin_fma((double)f[k], (double)f[k], squares);
+}
+template <bool BF16>
+__device__ __forceinline__ void add_squares(const Eight<BF16>& h, SumOf<BF16>& squares) {
+    float f[8];
+    floats(h, f);
+    if constexpr (BF16) {
+        float s[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] = __builtin_fmaf(f[k], f[k], f[k + 4] * f[k + 4]);
+        squares += (s[0] + s[1]) + (s[2] + s[3]);
+    } else {
+        add_wide_squares(h, squares);
+    }
 }
 template <class T>
 __device__ __forceinline__ bool beyond(T squares) { return !(squares < (T)__builtin_inff()); }
@@ -222,13 +226,15 @@ __global__ __launch_bounds__(64 * (WAVES < 4 ? 4 : WAVES)) void norm_rows_kernel
     for (int i = 0; i < GROUPS; ++i) add_squares(h[i], squares);
     squares = sum_of_row<WAVES>(squares, part, wave);
     double inverse = inverse_root(squares, p.cols, p.eps);
-    if (WAVES == 1 || kRows == 1 ? beyond(squares) : __syncthreads_or(beyond(squares))) {  // rare
-        double wide = 0.0;
+    if constexpr (BF16) {
+        if (WAVES == 1 || kRows == 1 ? beyond(squares) : __syncthreads_or(beyond(squares))) {  // rare
+            double wide = 0.0;
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) add_wide_squares(h[i], wide);
-        if (WAVES > 1) __syncthreads();  // the sums before have been read
-        wide = sum_of_row<WAVES>(wide, part, wave);
-        if (beyond(squares)) inverse = inverse_root(wide, p.cols, p.eps);
+            for (int i = 0; i < GROUPS; ++i) add_wide_squares(h[i], wide);
+            if (WAVES > 1) __syncthreads();  // the sums before have been read
+            wide = sum_of_row<WAVES>(wide, part, wave);
+            if (beyond(squares)) inverse = inverse_root(wide, p.cols, p.eps);
+        }
     }
     if (!valid) return;
 #pragma unroll
@@ -272,7 +278,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const NormArgs p) 
     }
     squares = sum_of_row<16>(squares, part, wave);
     double inverse = inverse_root(squares, p.cols, p.eps);
-    if (beyond(squares)) {  // rare
+    if (BF16 && beyond(squares)) {  // rare
         double wide = 0.0;
         for (int g = wave; g < groups; g += 16) add_wide_squares(load(g * kFp4Group + lane * 8, false), wide);
         __syncthreads();  // the sums before have been read
